@@ -13,9 +13,9 @@
  *   - Tensor arguments are DEVICE pointers owned by the caller, contiguous (row-major) in
  *     the stated layout, 16-byte aligned.  The library keeps no pointer after a call returns,
  *     except for the arena and the shape's optional lens array handed to vlc_cache_create
- *     (lens is read again by every vlc_topk_compact on that cache).
+ *     (lens is read again by every vlc_topk_compact on that cache), and the arena handed to vlc_pages_create.
  *   - Every call only enqueues work on the given HIP stream and returns; no call
- *     synchronises, allocates or frees device memory (vlc_cache_status synchronises, and says so).
+ *     synchronises, allocates or frees device memory (vlc_cache_status and vlc_pages_status synchronise, and say so).
  *   - Calls return a vlc_status; nothing throws or aborts.  vlc_last_error_string() holds a
  *     description of the calling thread's last failure.
  *   - Errors that only the device can see (a budget outside [1, m], a cache arena too
@@ -390,6 +390,130 @@ vlc_status vlc_decode_attn(vlc_cache* cache, int32_t layer_begin, int32_t layer_
 vlc_status vlc_decode_attn_steps(vlc_cache* cache, int32_t layer_begin, int32_t layer_end, int32_t n_steps,
                                  const void* q, const void* k_new, const void* v_new,
                                  const float* sm_scale, void* out, vlc_stream stream);
+
+/*
+ * The paged prompt cache.  A prompt that arrives in chunks is kept, before it is compressed, in a pool of pages of
+ * page_slots token slots each; the caller's table names the pages of every request in order, so requests grow without
+ * moving and without gaps of more than a page.  A chunk's rows are written (and quantised) by vlc_pages_write, or by the
+ * vlc_pages_attn call that attends over them; the attention of the last chunk, the post-vision window, hands out the row
+ * statistics that vlc_score_from_stats takes, and vlc_pages_read gives back the K and V that it and vlc_topk_compact take.
+ * Every layer has the same pages: page p of the table holds the tokens' rows of all layers and KV heads.
+ *
+ * Formats of a page's rows (vlc_pages_shape.format); quantised rows need bf16 storage (VLC_ERR_DTYPE otherwise):
+ *   VLC_PAGES_PLAIN  the storage type itself
+ *   VLC_PAGES_FP8    OCP E4M3 codes and one fp32 scale per row, as in the FP8 compressed cache:
+ *                    scale = absmax / 448, code = nearest E4M3 value to fp32(x / scale), ties to even
+ *   VLC_PAGES_INT8   signed 8-bit codes and one fp32 scale per row: scale = absmax / 127, code = nearest integer to
+ *                    fp32(x / scale), ties to even
+ * The scale of a row of zeros is 1, that of a row with an infinite or NaN entry is NaN (it reads back as NaN).
+ *
+ * Supported: d in {64, 128}; Hq % Hkv == 0 with g <= 8; L <= 1024; page_slots one of 16, 32, 64, 128, 256;
+ * n_pages * page_slots <= 2^30. */
+typedef enum { VLC_PAGES_PLAIN = 0, VLC_PAGES_FP8 = 1, VLC_PAGES_INT8 = 2 } vlc_pages_format;
+typedef struct {
+    int32_t L, Hq, Hkv, d;
+    int32_t page_slots, n_pages;
+    int32_t dtype;             /* vlc_dtype of the rows handed in and out, of the queries and of the outputs */
+    int32_t format;            /* vlc_pages_format */
+    int32_t reserved[4];       /* 0 */
+} vlc_pages_shape;
+
+/* The caller owns one device arena of vlc_pages_bytes(shape) bytes, 256-byte aligned.  Where things live inside it (byte
+ * offsets): the K row of (layer l, page p, KV head h, slot r) starts at k_off + (((l * n_pages + p) * Hkv + h) * page_slots
+ * + r) * d * elem_size, elem_size being 1 for quantised rows; the V row at v_off plus the same; their scales at
+ * k_scale_off / v_scale_off + (((l * n_pages + p) * Hkv + h) * page_slots + r) * 4.  vlc_pages_destroy frees host
+ * bookkeeping only.
+ * vlc_pages_clear must be enqueued once before any other call on the arena: it resets the sticky status and the counters of
+ * the attention, and leaves the pages' rows alone. */
+typedef struct vlc_pages vlc_pages;
+typedef struct {
+    size_t status_off;         /* int32[4]: sticky vlc_status, request, kind (-1: page, -2: lengths), detail */
+    size_t counters_off;
+    size_t k_off, v_off;
+    size_t k_scale_off, v_scale_off;   /* quantised formats only */
+    size_t total_bytes;
+} vlc_pages_layout;
+size_t     vlc_pages_bytes(const vlc_pages_shape* shape);
+vlc_status vlc_pages_create(const vlc_pages_shape* shape, void* arena, size_t arena_bytes, vlc_pages** out);
+void       vlc_pages_destroy(vlc_pages* pages);
+vlc_status vlc_pages_get_layout(const vlc_pages* pages, vlc_pages_layout* out);
+vlc_status vlc_pages_clear(vlc_pages* pages, vlc_stream stream);
+/* Synchronises the stream and returns the sticky device-side status of the calls so far. */
+vlc_status vlc_pages_status(vlc_pages* pages, vlc_stream stream);
+
+/* The requests of one call.  Request b holds n_b tokens once the call's c_b new ones are counted: row i of its chunk
+ * is position n_b - c_b + i, and position t lives in slot t % page_slots of page table[b][t / page_slots].
+ *   table    DEVICE int32 [B][max_pages]; entries of positions >= n_b are never read as pages
+ *   lens     DEVICE int32 [B][2] = (n_b, c_b), 0 <= c_b <= max_new, c_b <= n_b <= max_len; or NULL: (max_len, max_new)
+ *            for every request.  A request may have no new tokens (c_b = 0), or be empty.
+ *   max_new  rows per request in the chunk's tensors; max_len bounds n_b and sizes the launch (a captured graph whose
+ *            lens grow from replay to replay takes the largest):  1 <= max_new <= max_len <= max_pages * page_slots
+ * Both arrays are read when a call's kernels run.  A request whose lengths break these bounds is skipped, an entry of the
+ * table outside [0, n_pages) is taken as page 0 for reading (that request's results are then meaningless) and not written
+ * to; either sets the sticky status to VLC_ERR_INVALID_ARG.  Requests may share pages that no call writes to; two rows
+ * written to one slot by one call leave it undefined. */
+typedef struct {
+    int32_t B, max_pages, max_new, max_len;
+    const int32_t* table;
+    const int32_t* lens;
+    int32_t reserved[2];       /* 0 */
+} vlc_chunk;
+
+/* Rows of a tensor [layers in range, B, heads, rows, d]: the element strides of the first four, d itself being contiguous.
+ * data is 16-byte aligned, the strides are non-negative and multiples of 16 bytes.  K, V [B,L,Hkv,m,d] and what a projection
+ * leaves, [B,rows,heads,d] per layer, or a slice of it, are taken as they are.  Outputs must not overlap. */
+typedef struct {
+    void* data;
+    int64_t layer, request, head, row;
+} vlc_rows;
+
+/*
+ * vlc_pages_write -- the c_b new rows of K and V of every request into its pages, layers [layer_begin, layer_end),
+ * quantised if the pages are.  k_new, v_new: [layers in range, B, Hkv, max_new, d], storage dtype; rows >= c_b are not read.
+ * B * layers in range * Hkv <= 65535 here and in the two calls below.
+ */
+vlc_status vlc_pages_write(vlc_pages* pages, const vlc_chunk* chunk, int32_t layer_begin, int32_t layer_end,
+                           const vlc_rows* k_new, const vlc_rows* v_new, vlc_stream stream);
+
+/*
+ * vlc_pages_read -- positions [first, min(n_b, first + count)) of every request, as rows 0.. of k_out and v_out
+ * [layers in range, B, Hkv, count, d], storage dtype: the row itself, or fp32(code * scale) rounded to nearest even.  Rows
+ * beyond a request's are left as they are.  first >= 0, 1 <= count; chunk->max_new and c_b play no part.
+ */
+vlc_status vlc_pages_read(vlc_pages* pages, const vlc_chunk* chunk, int32_t layer_begin, int32_t layer_end,
+                          int32_t first, int32_t count, const vlc_rows* k_out, const vlc_rows* v_out, vlc_stream stream);
+
+/*
+ * vlc_pages_attn -- attention of a chunk of new tokens over what the pages hold of their request, layers [layer_begin,
+ * layer_end): one token (decoding), a few (drafted tokens to verify), or the thousands of a prompt's chunk.  If k_new !=
+ * NULL the new rows are written first, as by vlc_pages_write; else they are in the pages already.
+ *
+ *   s_ij = sm_scale[l] * <q[l,b,h,i,:], K_j>,  j <= n_b - c_b + i,  K_j and V_j as the pages hold them (code * scale)
+ *   out[l,b,h,i,:] = sum_j exp(s_ij - M_i) V_j / Z_i,   M_i = max_j s_ij,  Z_i = sum_j exp(s_ij - M_i)
+ *
+ * A position that a row does not see has no influence on it, whatever it holds.  Logits of -inf weigh nothing; a row with
+ * nothing else is 0 with M = -inf, Z = 0.
+ * q, out       [layers in range, B, Hq, max_new, d], storage dtype; rows >= c_b are not read / left as they are
+ * k_new, v_new [layers in range, B, Hkv, max_new, d], or both NULL
+ * sm_scale     [L] float (indexed by absolute layer), any finite numbers, or NULL for 1/sqrt(d)
+ * stats        NULL, or where to put M (natural-log domain) and Z of each row: fp32 [layers in range, B, Hq, max_new], rows
+ *              contiguous, the other strides (in floats) given.  With B requests' windows as the chunk these are the
+ *              row_max and row_sum that vlc_score_from_stats takes.
+ * workspace    scratch of at least vlc_pages_attn_workspace_bytes bytes (may be NULL when that is 0).  Calls on one
+ *              vlc_pages that may overlap on the device race, as those on one vlc_cache do.
+ * Accumulation and statistics are fp32; bf16 storage rounds the probabilities to bf16 for the product with V, fp32 storage
+ * does not.
+ */
+typedef struct {
+    float* row_max;
+    float* row_sum;
+    int64_t layer, request, head;
+} vlc_row_stats;
+vlc_status vlc_pages_attn_workspace_bytes(const vlc_pages* pages, const vlc_chunk* chunk, int32_t n_layers, size_t* bytes_out);
+vlc_status vlc_pages_attn(vlc_pages* pages, const vlc_chunk* chunk, int32_t layer_begin, int32_t layer_end,
+                          const vlc_rows* q, const vlc_rows* k_new, const vlc_rows* v_new, const float* sm_scale,
+                          const vlc_rows* out, const vlc_row_stats* stats, void* workspace, size_t workspace_bytes,
+                          vlc_stream stream);
 
 /*
  * vlc_probe_read_stream -- measurement aid, not a step of the path: one kernel that reads `bytes` bytes of

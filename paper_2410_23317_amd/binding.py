@@ -49,6 +49,32 @@ class vlc_cache_options(C.Structure):
                [("reserved", C.c_int32 * 7)]
 
 
+VLC_PAGES_PLAIN, VLC_PAGES_FP8, VLC_PAGES_INT8 = 0, 1, 2
+
+
+class vlc_pages_shape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("L", "Hq", "Hkv", "d", "page_slots", "n_pages", "dtype", "format")] + \
+               [("reserved", C.c_int32 * 4)]
+
+
+class vlc_pages_layout(C.Structure):
+    _fields_ = [(n, C.c_size_t) for n in ("status_off", "counters_off", "k_off", "v_off", "k_scale_off", "v_scale_off",
+                                          "total_bytes")]
+
+
+class vlc_chunk(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "max_pages", "max_new", "max_len")] + \
+               [("table", C.c_void_p), ("lens", C.c_void_p), ("reserved", C.c_int32 * 2)]
+
+
+class vlc_rows(C.Structure):
+    _fields_ = [("data", C.c_void_p)] + [(n, C.c_int64) for n in ("layer", "request", "head", "row")]
+
+
+class vlc_row_stats(C.Structure):
+    _fields_ = [("row_max", C.c_void_p), ("row_sum", C.c_void_p)] + [(n, C.c_int64) for n in ("layer", "request", "head")]
+
+
 def _load() -> C.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built: run `python -c 'import __graft_entry__ as g; g.build()'` "
@@ -106,6 +132,26 @@ def _load() -> C.CDLL:
     lib.vlc_decode_attn.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp, vp]
     lib.vlc_decode_attn_steps.restype = C.c_int
     lib.vlc_decode_attn_steps.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp, vp]
+    pgs, chk, rows = C.POINTER(vlc_pages_shape), C.POINTER(vlc_chunk), C.POINTER(vlc_rows)
+    lib.vlc_pages_bytes.restype = sz
+    lib.vlc_pages_bytes.argtypes = [pgs]
+    lib.vlc_pages_create.restype = C.c_int
+    lib.vlc_pages_create.argtypes = [pgs, vp, sz, C.POINTER(vp)]
+    lib.vlc_pages_destroy.restype = None
+    lib.vlc_pages_destroy.argtypes = [vp]
+    lib.vlc_pages_get_layout.restype = C.c_int
+    lib.vlc_pages_get_layout.argtypes = [vp, C.POINTER(vlc_pages_layout)]
+    for name in ("vlc_pages_clear", "vlc_pages_status"):
+        getattr(lib, name).restype = C.c_int
+        getattr(lib, name).argtypes = [vp, vp]
+    lib.vlc_pages_write.restype = C.c_int
+    lib.vlc_pages_write.argtypes = [vp, chk, i32, i32, rows, rows, vp]
+    lib.vlc_pages_read.restype = C.c_int
+    lib.vlc_pages_read.argtypes = [vp, chk, i32, i32, i32, i32, rows, rows, vp]
+    lib.vlc_pages_attn_workspace_bytes.restype = C.c_int
+    lib.vlc_pages_attn_workspace_bytes.argtypes = [vp, chk, i32, C.POINTER(sz)]
+    lib.vlc_pages_attn.restype = C.c_int
+    lib.vlc_pages_attn.argtypes = [vp, chk, i32, i32, rows, rows, rows, vp, rows, C.POINTER(vlc_row_stats), vp, sz, vp]
     lib.vlc_probe_read_stream.restype = C.c_int
     lib.vlc_probe_read_stream.argtypes = [vp, sz, vp, i32, vp]
     return lib
@@ -313,3 +359,140 @@ def vlc_probe_read_stream(buf, sink, blocks) -> None:
 def vlc_decode_attn_steps(cache: Cache, layer_begin, layer_end, n_steps, q, k_new, v_new, sm_scale, out) -> None:
     _check(lib.vlc_decode_attn_steps(cache.handle, int(layer_begin), int(layer_end), int(n_steps), _ptr(q),
                                      _ptr(k_new), _ptr(v_new), _ptr(sm_scale), _ptr(out), _stream()))
+
+
+# ---- the paged prompt cache ---------------------------------------------------------------------------------------
+_PAGE_FORMATS = {"plain": VLC_PAGES_PLAIN, "fp8": VLC_PAGES_FP8, "int8": VLC_PAGES_INT8}
+
+
+def make_pages_shape(L, Hq, Hkv, d, page_slots, n_pages, dtype, format="plain") -> vlc_pages_shape:
+    code = {torch.float32: VLC_F32, torch.bfloat16: VLC_BF16, "f32": VLC_F32, "bf16": VLC_BF16}.get(dtype, dtype)
+    return vlc_pages_shape(L, Hq, Hkv, d, page_slots, n_pages, code, _PAGE_FORMATS.get(format, format))
+
+
+def vlc_pages_bytes(shape: vlc_pages_shape) -> int:
+    n = lib.vlc_pages_bytes(C.byref(shape))
+    if n == 0:
+        raise VlcError(VLC_ERR_INVALID_ARG, vlc_last_error_string())
+    return n
+
+
+class Pages:
+    """Owns the arena tensor of a paged prompt cache and the library's host-side handle; cleared on the current stream."""
+
+    def __init__(self, shape: vlc_pages_shape, device="cuda"):
+        self.handle = None
+        self.shape = shape
+        nbytes = vlc_pages_bytes(shape)
+        self.arena = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        handle = C.c_void_p()
+        _check(lib.vlc_pages_create(C.byref(shape), self.arena.data_ptr(), nbytes, C.byref(handle)))
+        self.handle = handle
+        self.layout = vlc_pages_layout()
+        _check(lib.vlc_pages_get_layout(self.handle, C.byref(self.layout)))
+        vlc_pages_clear(self)
+
+    def close(self) -> None:
+        if self.handle:
+            lib.vlc_pages_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def vlc_pages_create(shape: vlc_pages_shape, device="cuda") -> Pages:
+    return Pages(shape, device)
+
+
+def vlc_pages_clear(pages: Pages) -> None:
+    _check(lib.vlc_pages_clear(pages.handle, _stream()))
+
+
+def vlc_pages_status(pages: Pages) -> None:
+    """Synchronises the stream; raises VlcError if the device flagged lengths or a page out of range."""
+    _check(lib.vlc_pages_status(pages.handle, _stream()))
+
+
+def make_chunk(table: torch.Tensor, max_new: int, max_len: int, lens: Optional[torch.Tensor] = None) -> vlc_chunk:
+    """table: int32 device tensor [B, max_pages]; lens: optional int32 device tensor [B, 2] of (n_b, c_b).  Both stay alive
+    with the returned structure."""
+    if table.dtype != torch.int32 or table.dim() != 2:
+        raise ValueError("table must be an int32 tensor [B, max_pages]")
+    if lens is not None and (lens.dtype != torch.int32 or tuple(lens.shape) != (table.shape[0], 2)):
+        raise ValueError("lens must be an int32 tensor [B, 2]")
+    c = vlc_chunk(table.shape[0], table.shape[1], int(max_new), int(max_len), _ptr(table), _ptr(lens))
+    c.tensors = (table, lens)
+    return c
+
+
+def _rows(t: Optional[torch.Tensor], name: str, pages: Pages, dims) -> Optional[vlc_rows]:
+    """vlc_rows of a tensor [layers, B, heads, rows, d] of any strides, d contiguous."""
+    if t is None:
+        return None
+    dt = torch.float32 if pages.shape.dtype == VLC_F32 else torch.bfloat16
+    if t.dtype != dt or tuple(t.shape) != tuple(dims):
+        raise ValueError(f"{name} must be {dt} of shape {tuple(dims)}, not {t.dtype} {tuple(t.shape)}")
+    if t.device != pages.arena.device or t.stride(4) != 1:
+        raise ValueError(f"{name} must lie on {pages.arena.device} with its last dimension contiguous")
+    return vlc_rows(t.data_ptr(), *t.stride()[:4])
+
+
+def _pages_stream(pages: Pages) -> int:
+    if pages.arena.device.index != torch.cuda.current_device():
+        raise ValueError(f"the pages lie on {pages.arena.device}, which is not the current device")
+    return _stream()
+
+
+def _ref(r):
+    return None if r is None else C.byref(r)
+
+
+def vlc_pages_write(pages: Pages, chunk: vlc_chunk, layer_begin, layer_end, k_new, v_new) -> None:
+    s = pages.shape
+    dims = (layer_end - layer_begin, chunk.B, s.Hkv, chunk.max_new, s.d)
+    k, v = _rows(k_new, "k_new", pages, dims), _rows(v_new, "v_new", pages, dims)
+    _check(lib.vlc_pages_write(pages.handle, C.byref(chunk), int(layer_begin), int(layer_end), _ref(k), _ref(v), _pages_stream(pages)))
+
+
+def vlc_pages_read(pages: Pages, chunk: vlc_chunk, layer_begin, layer_end, first, k_out, v_out) -> None:
+    """Reads as many positions from `first` on as k_out and v_out [layers, B, Hkv, count, d] have rows."""
+    s = pages.shape
+    count = k_out.shape[3]
+    dims = (layer_end - layer_begin, chunk.B, s.Hkv, count, s.d)
+    k, v = _rows(k_out, "k_out", pages, dims), _rows(v_out, "v_out", pages, dims)
+    _check(lib.vlc_pages_read(pages.handle, C.byref(chunk), int(layer_begin), int(layer_end), int(first), int(count), _ref(k), _ref(v),
+                              _pages_stream(pages)))
+
+
+def vlc_pages_attn_workspace_bytes(pages: Pages, chunk: vlc_chunk, n_layers) -> int:
+    n = C.c_size_t(0)
+    _check(lib.vlc_pages_attn_workspace_bytes(pages.handle, C.byref(chunk), int(n_layers), C.byref(n)))
+    return n.value
+
+
+def vlc_pages_attn(pages: Pages, chunk: vlc_chunk, layer_begin, layer_end, q, k_new, v_new, sm_scale, out, row_max, row_sum,
+                   workspace) -> None:
+    """q, out [layers, B, Hq, max_new, d]; k_new, v_new [layers, B, Hkv, max_new, d] or None; row_max, row_sum fp32
+    [layers, B, Hq, max_new] of equal strides, or None."""
+    s = pages.shape
+    n = layer_end - layer_begin
+    qd, kd = (n, chunk.B, s.Hq, chunk.max_new, s.d), (n, chunk.B, s.Hkv, chunk.max_new, s.d)
+    stats = None
+    if (row_max is None) != (row_sum is None):
+        raise ValueError("row_max and row_sum come together")
+    if row_max is not None:
+        for t in (row_max, row_sum):
+            if t.dtype != torch.float32 or tuple(t.shape) != qd[:4] or t.device != pages.arena.device:
+                raise ValueError(f"row_max and row_sum must be fp32 of shape {qd[:4]} on {pages.arena.device}")
+        if row_max.stride() != row_sum.stride() or (chunk.max_new > 1 and row_max.stride(3) != 1):
+            raise ValueError("row_max and row_sum must have equal strides and contiguous rows")
+        stats = vlc_row_stats(row_max.data_ptr(), row_sum.data_ptr(), *row_max.stride()[:3])
+    qr, o = _rows(q, "q", pages, qd), _rows(out, "out", pages, qd)
+    k, v = _rows(k_new, "k_new", pages, kd), _rows(v_new, "v_new", pages, kd)
+    _check(lib.vlc_pages_attn(pages.handle, C.byref(chunk), int(layer_begin), int(layer_end), _ref(qr), _ref(k), _ref(v), _ptr(sm_scale),
+                              _ref(o), _ref(stats), _ptr(workspace),
+                              0 if workspace is None else workspace.numel() * workspace.element_size(), _pages_stream(pages)))

@@ -13,8 +13,10 @@
 #include "internal.h"
 
 namespace {
-
 thread_local char g_err[512] = "";
+}  // namespace
+
+namespace vlc {
 
 vlc_status fail(vlc_status st, const char* fmt, ...) {
     va_list ap;
@@ -27,6 +29,13 @@ vlc_status fail(vlc_status st, const char* fmt, ...) {
 vlc_status hip_fail(hipError_t e, const char* where) {
     return fail(VLC_ERR_HIP, "%s: %s", where, hipGetErrorString(e));
 }
+
+}  // namespace vlc
+
+namespace {
+
+using vlc::fail;
+using vlc::hip_fail;
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 

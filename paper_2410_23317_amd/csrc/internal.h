@@ -10,6 +10,10 @@
 
 namespace vlc {
 
+// The calling thread's last failure, as vlc_last_error_string reports it.
+vlc_status fail(vlc_status st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+vlc_status hip_fail(hipError_t e, const char* where);
+
 constexpr int kMaxLayers = 1024;
 constexpr int kScoreChunk = 256;       // keys per block of the generic scoring sweeps
 constexpr int kReaderStride = 64;      // ints between the ticket counters of two layers: a cache line each (measured: counters that share a
@@ -73,6 +77,17 @@ struct CacheDev {                      // device pointers into the caller's aren
     float* scales;                     // FP8 caches: one fp32 scale per K row and per V row, laid out like the rows
 };
 
+// ---- the paged prompt cache ----
+struct PagesDev {                      // device pointers into the caller's arena
+    int32_t* status;                   // [4]
+    int32_t* counters;                 // [kMaxPagesRows] key splits of a row that have left their partial result
+    char* k;
+    char* v;
+    float* k_scale;                    // quantised formats
+    float* v_scale;
+};
+constexpr int kMaxPagesRows = 65536;   // (layer, request, kv head) rows of one call: 65535 at most
+
 }  // namespace vlc
 
 struct vlc_cache {
@@ -89,6 +104,13 @@ struct vlc_cache {
     int32_t num_cus;                   // compute units of the device the cache was created on
     bool ragged;                       // the last compaction had per-request lengths (dev.lens is valid)
     int32_t appended[vlc::kMaxLayers]; // decode appends enqueued so far, per layer (the device keeps the count the kernels use)
+};
+
+struct vlc_pages {
+    vlc_pages_shape shape;
+    vlc_pages_layout layout;
+    vlc::PagesDev dev;
+    int32_t num_cus;                   // compute units of the device that is current when the handle is created
 };
 
 namespace vlc {
@@ -168,6 +190,28 @@ struct DecodeArgs {
     hipStream_t stream;
 };
 hipError_t launch_decode(const DecodeArgs& a);
+
+// ---- the paged prompt cache (api_pages.hip, pages.hip, pages_attn*.hip) ----
+
+// One call on the pages: what every kernel of it needs.
+struct PagesCall {
+    vlc_pages_shape s;
+    PagesDev dev;
+    vlc_chunk chunk;
+    int layer_begin, n_layers;
+    hipStream_t stream;
+};
+hipError_t launch_pages_clear(const PagesDev& dev, hipStream_t st);
+hipError_t launch_pages_write(const PagesCall& c, const vlc_rows& k_new, const vlc_rows& v_new);
+hipError_t launch_pages_read(const PagesCall& c, int first, int count, const vlc_rows& k_out, const vlc_rows& v_out);
+struct PagesAttn {
+    PagesCall c;
+    vlc_rows q, out;
+    const float* sm_scale;             // may be null
+    vlc_row_stats stats;               // row_max null: none
+    void* workspace;
+};
+hipError_t launch_pages_attn_simple(const PagesAttn& a);
 
 // ---- measurement aid: a kernel that only reads `bytes` bytes (a multiple of 16) once
 hipError_t launch_read_stream(const void* buf, size_t bytes, uint32_t* sink, int blocks, hipStream_t st);

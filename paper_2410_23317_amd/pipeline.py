@@ -5,6 +5,8 @@ in the middle in one launch (vlc_sparsity_allocate).
 Fused route for the scores: vlc_window_attn (attention of the window rows + row statistics) ->
 vlc_score_from_stats (column sweep only).
 Every decode step: vlc_decode_attn over a layer range of the compressed cache.
+Prompts that arrive in chunks (PagedPrompt): vlc_pages_attn per chunk and layer range; after the last chunk, the window,
+vlc_pages_read -> vlc_score_from_stats -> vlc_sparsity_allocate -> vlc_topk_compact.
 """
 from __future__ import annotations
 
@@ -122,6 +124,79 @@ class VLCachePath:
         V.vlc_score(t["shape"], q_next, k, sm_scale, self.p, t["scores"], t["row_max"], t["row_sum"], None, t["workspace"])
         V.vlc_cache_hit_rate(self.cache, t["scores"], t["hits"], t["rate"])
         return t["hits"], t["rate"], t["scores"]
+
+
+class PagedPrompt:
+    """A batch of prompts that arrive in chunks, kept in pages until they are compressed.
+
+    page_table [B, max_pages] names the pages of each request (int32, on the device); by default request b owns pages
+    b * max_pages .. of a pool with room for max_len tokens each.  The host keeps how many tokens each request holds."""
+
+    def __init__(self, L: int, Hq: int, Hkv: int, d: int, dtype, B: int, max_len: int, page_slots: int = 64, format="plain",
+                 n_pages: Optional[int] = None, page_table: Optional[torch.Tensor] = None, device: str = "cuda"):
+        max_pages = -(-max_len // page_slots)
+        self.max_len = int(max_len)
+        if page_table is None:
+            page_table = torch.arange(B * max_pages, dtype=torch.int32, device=device).view(B, max_pages)
+        self.table = page_table
+        self.pages = V.vlc_pages_create(V.make_pages_shape(L, Hq, Hkv, d, page_slots, n_pages or B * max_pages, dtype, format), device)
+        self.tokens = [0] * B
+        self.device = torch.device(device)
+        self.workspace = None
+        self.chunk = None
+
+    def begin_chunk(self, new_tokens) -> V.vlc_chunk:
+        """The next chunk brings new_tokens[b] tokens to request b (0: none): the lengths that extend() and the calls on
+        self.chunk take from here on."""
+        new = [int(c) for c in new_tokens]
+        if len(new) != len(self.tokens) or min(new) < 0 or max(new) < 1:
+            raise ValueError("new_tokens: a count for each request, none negative and not all zero")
+        total = [n + c for n, c in zip(self.tokens, new)]
+        if max(total) > self.max_len:
+            raise ValueError(f"a request would hold {max(total)} tokens, {self.max_len} were provided for")
+        self.tokens = total
+        lens = torch.tensor(list(zip(total, new)), dtype=torch.int32).to(self.device)
+        self.chunk = V.make_chunk(self.table, max(new), max(total), lens)
+        return self.chunk
+
+    def extend(self, layer_begin, layer_end, q, k_new, v_new, sm_scale, out, row_max=None, row_sum=None) -> None:
+        """The chunk's rows of layers [layer_begin, layer_end) into the pages, and their attention."""
+        need = V.vlc_pages_attn_workspace_bytes(self.pages, self.chunk, layer_end - layer_begin)
+        if need and (self.workspace is None or self.workspace.numel() < need):
+            self.workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+        V.vlc_pages_attn(self.pages, self.chunk, layer_begin, layer_end, q, k_new, v_new, sm_scale, out, row_max, row_sum, self.workspace)
+
+    def read(self, k_out, v_out) -> None:
+        """Every request's K and V so far, into tensors [B, L, Hkv, m, d]; rows beyond a request's are left as they are."""
+        V.vlc_pages_read(self.pages, self.chunk, 0, self.pages.shape.L, 0, k_out.transpose(0, 1), v_out.transpose(0, 1))
+
+    def compress(self, path: VLCachePath, q_win, sm_scale, k_out, v_out) -> None:
+        """Compression of the prompts whose last chunk was the window and left its statistics in path.row_max and
+        path.row_sum (extend(.., row_max=path.row_max.transpose(0, 1), row_sum=..)); path.shape.lens, if the batch is
+        ragged, holds what self.chunk.lens holds."""
+        self.read(k_out, v_out)
+        path.score_from_stats(q_win, k_out, sm_scale)
+        V.vlc_sparsity_allocate(path.shape, path.nnz, path.gamma, path.alpha[0], path.alpha[1], path.k, path.beta)
+        path.topk_compact(k_out, v_out)
+
+    def status(self) -> None:
+        V.vlc_pages_status(self.pages)
+
+
+def pages_layer_view(pages: V.Pages, l: int):
+    """(K, V) of a layer as tensors [n_pages, Hkv, page_slots, d] aliasing the arena; of quantised pages the codes (uint8 for
+    FP8, int8), followed by the scales [n_pages, Hkv, page_slots] of both."""
+    s, lay, arena = pages.shape, pages.layout, pages.arena
+    dims = (s.n_pages, s.Hkv, s.page_slots)
+    rows = s.n_pages * s.Hkv * s.page_slots
+    dt = {V.VLC_PAGES_PLAIN: torch.float32 if s.dtype == V.VLC_F32 else torch.bfloat16, V.VLC_PAGES_FP8: torch.uint8,
+          V.VLC_PAGES_INT8: torch.int8}[s.format]
+    nb = rows * s.d * dt.itemsize
+    view = [arena[off + l * nb: off + (l + 1) * nb].view(dt).view(*dims, s.d) for off in (lay.k_off, lay.v_off)]
+    if s.format != V.VLC_PAGES_PLAIN:
+        view += [arena[off + l * rows * 4: off + (l + 1) * rows * 4].view(torch.float32).view(dims)
+                 for off in (lay.k_scale_off, lay.v_scale_off)]
+    return tuple(view)
 
 
 def cache_layer_view(cache: V.Cache, b: int, l: int, appended: int = 0):

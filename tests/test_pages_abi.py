@@ -1,0 +1,166 @@
+"""The paged prompt cache without a GPU: validation on the host, the arena's layout, and the definitions the GPU tests
+compare with against the oracle."""
+import ctypes as C
+import os
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import vlcache_oracle as O
+
+import pages_util as U
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def V():
+    if not os.path.exists(os.path.join(ROOT, "paper_2410_23317_amd", "libvlcache.so")):
+        import __graft_entry__
+        __graft_entry__.build()
+    import paper_2410_23317_amd as V
+    return V
+
+
+BASE = dict(L=2, Hq=8, Hkv=2, d=128, page_slots=16, n_pages=40, dtype="bf16", format="plain")
+
+
+def create(V, **kw):
+    s = V.make_pages_shape(**{**BASE, **kw})
+    h = C.c_void_p()
+    n = V.lib.vlc_pages_bytes(C.byref(s))
+    st = V.lib.vlc_pages_create(C.byref(s), 4096, n, C.byref(h))
+    return s, n, h, st
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(Hq=7), "SHAPE"), (dict(Hq=18), "SHAPE"), (dict(d=96), "SHAPE"), (dict(L=0), "SHAPE"), (dict(L=1025), "SHAPE"),
+    (dict(page_slots=8), "SHAPE"), (dict(page_slots=48), "SHAPE"), (dict(page_slots=512), "SHAPE"), (dict(n_pages=0), "SHAPE"),
+    (dict(n_pages=(1 << 26) + 1), "SHAPE"), (dict(dtype=5), "DTYPE"), (dict(format=3), "INVALID_ARG"),
+    (dict(dtype="f32", format="fp8"), "DTYPE"), (dict(dtype="f32", format="int8"), "DTYPE"),
+])
+def test_shapes_are_refused(V, kw, code):
+    s, n, h, st = create(V, **kw)
+    assert n == 0 and st == getattr(V, "VLC_ERR_" + code) and not h.value and V.vlc_last_error_string()
+
+
+@pytest.mark.parametrize("fmt,dtype,es", [("plain", "bf16", 2), ("plain", "f32", 4), ("fp8", "bf16", 1), ("int8", "bf16", 1)])
+def test_layout(V, fmt, dtype, es):
+    s, n, h, st = create(V, format=fmt, dtype=dtype)
+    assert st == V.VLC_OK
+    lay = V.vlc_pages_layout()
+    assert V.lib.vlc_pages_get_layout(h, C.byref(lay)) == V.VLC_OK and lay.total_bytes == n
+    rows = 2 * 40 * 2 * 16
+    assert lay.v_off - lay.k_off == rows * 128 * es and lay.k_off % 256 == 0
+    if es == 1:
+        assert lay.v_scale_off - lay.k_scale_off == rows * 4 and n >= lay.v_scale_off + rows * 4
+    else:
+        assert n >= lay.v_off + rows * 128 * es
+    V.lib.vlc_pages_destroy(h)
+    bad = C.c_void_p()
+    assert V.lib.vlc_pages_create(C.byref(s), 4096, n - 1, C.byref(bad)) == V.VLC_ERR_CAPACITY
+    assert V.lib.vlc_pages_create(C.byref(s), 4096 + 16, n, C.byref(bad)) == V.VLC_ERR_INVALID_ARG
+    assert V.lib.vlc_pages_create(C.byref(s), None, n, C.byref(bad)) == V.VLC_ERR_INVALID_ARG
+    assert V.lib.vlc_pages_create(C.byref(s), 4096, n, None) == V.VLC_ERR_INVALID_ARG
+    s.reserved[2] = 1
+    assert V.lib.vlc_pages_bytes(C.byref(s)) == 0
+
+
+def chunk_of(V, **kw):
+    f = dict(B=2, max_pages=20, max_new=5, max_len=300, table=4096, lens=None)
+    f.update(kw)
+    return V.vlc_chunk(f["B"], f["max_pages"], f["max_new"], f["max_len"], f["table"], f["lens"])
+
+
+def rows_of(V, **kw):
+    f = dict(data=8192, layer=1 << 20, request=1 << 16, head=1 << 12, row=128)
+    f.update(kw)
+    return V.vlc_rows(f["data"], f["layer"], f["request"], f["head"], f["row"])
+
+
+def test_calls_are_refused_before_any_launch(V):
+    s, n, h, st = create(V)
+    ok_chunk, r, lib = chunk_of(V), rows_of(V), V.lib
+    R, K = C.byref(r), C.byref(ok_chunk)
+
+    def write(h=h, chunk=K, lb=0, le=2, k=R, v=R):
+        return lib.vlc_pages_write(h, chunk, lb, le, k, v, None)
+
+    def read(h=h, chunk=K, lb=0, le=2, first=0, count=10, k=R, v=R):
+        return lib.vlc_pages_read(h, chunk, lb, le, first, count, k, v, None)
+
+    def attn(h=h, chunk=K, lb=0, le=2, q=R, k=None, v=None, out=R, stats=None, ws=None, n=0):
+        return lib.vlc_pages_attn(h, chunk, lb, le, q, k, v, None, out, stats, ws, n, None)
+
+    inv, shp, cap = V.VLC_ERR_INVALID_ARG, V.VLC_ERR_SHAPE, V.VLC_ERR_CAPACITY
+    for call in (write, read, attn):
+        assert call(h=None) == inv and call(chunk=None) == inv
+        for lb, le in ((-1, 1), (0, 3), (1, 1), (2, 1)):
+            assert call(lb=lb, le=le) == inv
+        for kw in (dict(table=None), dict(table=4098), dict(lens=4097)):
+            assert call(chunk=C.byref(chunk_of(V, **kw))) == inv, kw
+        for kw in (dict(B=0), dict(max_pages=0), dict(max_new=0), dict(max_new=301), dict(max_len=321), dict(B=16384, max_new=1)):
+            assert call(chunk=C.byref(chunk_of(V, **kw))) == shp, kw
+        reserved = chunk_of(V)
+        reserved.reserved[1] = 1
+        assert call(chunk=C.byref(reserved)) == inv
+    bad_rows = [dict(data=None), dict(data=8200), dict(row=-128), dict(row=130), dict(head=4), dict(request=-8), dict(layer=1 << 43)]
+    for kw in bad_rows:
+        b = C.byref(rows_of(V, **kw))
+        for st in (write(k=b), write(v=b), read(k=b), read(v=b), attn(q=b), attn(out=b), attn(k=b, v=R), attn(k=R, v=b)):
+            assert st == inv, kw
+    for kw in (dict(row=0), dict(head=0), dict(request=0), dict(layer=0)):          # outputs that fold onto themselves
+        b = C.byref(rows_of(V, **kw))
+        assert read(k=b) == inv and read(v=b) == inv and attn(out=b) == inv, kw
+    assert read(first=-1) == inv and read(count=0) == inv
+    assert read(first=300) == V.VLC_OK                                             # nobody has that position: nothing to launch
+    assert attn(k=R) == inv and attn(v=R) == inv
+    for kw in (dict(row_max=None), dict(row_sum=None), dict(head=4), dict(request=-5), dict(layer=0)):
+        f = {**dict(row_max=4096, row_sum=4096, layer=1000, request=100, head=5), **kw}
+        assert attn(stats=C.byref(V.vlc_row_stats(f["row_max"], f["row_sum"], f["layer"], f["request"], f["head"]))) == inv, kw
+    need = C.c_size_t(5)
+    assert lib.vlc_pages_attn_workspace_bytes(h, K, 2, None) == inv
+    assert lib.vlc_pages_attn_workspace_bytes(h, K, 3, C.byref(need)) == inv and need.value == 0
+    big = chunk_of(V, max_pages=4096, max_new=1, max_len=65536)
+    assert lib.vlc_pages_attn_workspace_bytes(h, C.byref(big), 1, C.byref(need)) == V.VLC_OK
+    if need.value:
+        assert attn(chunk=C.byref(big), le=1) == inv                               # no workspace
+        assert attn(chunk=C.byref(big), le=1, ws=4096, n=need.value - 1) == cap
+        assert attn(chunk=C.byref(big), le=1, ws=4100, n=need.value) == inv
+    assert lib.vlc_pages_clear(None, None) == inv and lib.vlc_pages_status(None, None) == inv
+    lib.vlc_pages_destroy(h)
+
+
+def test_formats_of_the_comparison_are_the_definitions():
+    rng = np.random.default_rng(3)
+    x = rng.standard_normal((200, 64)).astype(np.float32) * np.exp(rng.uniform(-20, 20, (200, 1))).astype(np.float32)
+    x[7] = 0
+    t = torch.from_numpy(x).to(torch.bfloat16)
+    code, scale = O.quantize_e4m3_rows(t.float().numpy())
+    want = O.dequantize_e4m3_rows(code, scale).astype(np.float64)
+    got = U.held(t, "fp8").numpy()
+    np.testing.assert_allclose(got, want, rtol=2.0 ** -23, atol=0)           # the oracle's product is rounded to fp32
+    ints, sc = U.codes_of(t, "int8")
+    assert float(ints.abs().max()) == 127 and sc[7] == 1 and bool((ints == ints.round()).all())
+    # within half a step and what the rounding of the quotient to fp32 adds, 2^-24 of at most 127
+    assert bool(((ints * sc - t.double()).abs() <= sc * (0.5 + 127 * 2.0 ** -24)).all())
+    bad = t.clone()
+    bad[3, 5] = float("inf")
+    bad[4, 0] = float("nan")
+    for fmt in ("fp8", "int8"):
+        h = U.held(bad, fmt)
+        assert bool(torch.isnan(h[3]).all()) and bool(torch.isnan(h[4]).all()) and bool(torch.isfinite(h[5:]).all())
+
+
+def test_attention_of_the_comparison_is_the_oracles():
+    g = torch.Generator().manual_seed(1)
+    q, k, v = (torch.randn(s, generator=g, dtype=torch.float64) for s in ((4, 9, 64), (2, 50, 64), (2, 50, 64)))
+    out, M, Z, A, _ = U.attention(q, k, v, 0.2, 50, 9)
+    o, m, z = O.window_attention(q.numpy(), k.numpy(), v.numpy(), 0.2)
+    np.testing.assert_allclose(out.numpy(), o, rtol=1e-12)
+    np.testing.assert_allclose(M.numpy(), m, rtol=1e-12)
+    np.testing.assert_allclose(Z.numpy(), z, rtol=1e-12)
+    v[0, 47, 3] = float("inf")                                                # seen by the chunk's rows 6 and up only
+    o2 = U.attention(q, k, v, 0.2, 50, 9)[0]
+    assert bool(torch.isinf(o2[:2, 6:, 3]).all()) and bool(torch.isfinite(o2[:2, :6]).all()) and bool((o2[2:] == out[2:]).all())
