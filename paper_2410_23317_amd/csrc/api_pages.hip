@@ -64,6 +64,8 @@ vlc_status check_call(const char* who, const vlc_pages* pages, const vlc_chunk* 
     if (c->max_new < 1 || c->max_new > c->max_len || c->max_len > (int64_t)c->max_pages * s.page_slots || c->max_len > 1 << 30)
         return fail(VLC_ERR_SHAPE, "%s: 1 <= max_new = %d <= max_len = %d <= max_pages * page_slots = %lld (and 2^30) does not hold", who,
                     c->max_new, c->max_len, (long long)c->max_pages * s.page_slots);
+    if ((double)c->B * n_layers * s.Hkv * (c->max_len / 1024 + 1) > 1.0e9)
+        return fail(VLC_ERR_SHAPE, "%s: B * layers * Hkv * max_len exceeds 10^12", who);
     if ((int64_t)c->max_new * s.Hq > 1 << 28) return fail(VLC_ERR_SHAPE, "%s: max_new * Hq = %lld exceeds 2^28", who, (long long)c->max_new * s.Hq);
     return VLC_OK;
 }
@@ -204,6 +206,8 @@ vlc_status vlc_pages_attn_workspace_bytes(const vlc_pages* pages, const vlc_chun
     *bytes_out = 0;
     if (vlc_status st = check_layers(who, pages, 0, n_layers)) return st;
     if (vlc_status st = check_call(who, pages, chunk, n_layers)) return st;
+    const vlc::PagesCall c = pages_call(pages, chunk, 0, n_layers, nullptr);
+    *bytes_out = vlc::pages_few_supported(c) ? vlc::pages_few_workspace_bytes(c) : 0;
     return VLC_OK;
 }
 
@@ -240,6 +244,14 @@ vlc_status vlc_pages_attn(vlc_pages* pages, const vlc_chunk* chunk, int32_t laye
     a.q = *q; a.out = *out; a.sm_scale = sm_scale; a.workspace = workspace;
     memset(&a.stats, 0, sizeof(a.stats));
     if (stats) a.stats = *stats;
+    memset(&a.k_new, 0, sizeof(a.k_new));
+    a.v_new = a.k_new;
+    if (k_new) { a.k_new = *k_new; a.v_new = *v_new; }
+    if (vlc::pages_few_supported(a.c)) {
+        const hipError_t e = vlc::launch_pages_few(a);
+        if (e != hipSuccess) return hip_fail(e, who);
+        return VLC_OK;
+    }
     if (k_new) {
         const hipError_t e = vlc::launch_pages_write(a.c, *k_new, *v_new);
         if (e != hipSuccess) return hip_fail(e, who);

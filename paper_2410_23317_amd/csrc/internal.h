@@ -206,12 +206,16 @@ hipError_t launch_pages_write(const PagesCall& c, const vlc_rows& k_new, const v
 hipError_t launch_pages_read(const PagesCall& c, int first, int count, const vlc_rows& k_out, const vlc_rows& v_out);
 struct PagesAttn {
     PagesCall c;
-    vlc_rows q, out;
+    vlc_rows q, k_new, v_new, out;     // k_new.data null: the chunk's rows are in the pages already
     const float* sm_scale;             // may be null
     vlc_row_stats stats;               // row_max null: none
     void* workspace;
 };
 hipError_t launch_pages_attn_simple(const PagesAttn& a);
+// at most 32 query rows per KV head (pages_attn_few.hip); writes the chunk's rows itself
+bool pages_few_supported(const PagesCall& c);
+size_t pages_few_workspace_bytes(const PagesCall& c);
+hipError_t launch_pages_few(const PagesAttn& a);
 
 // ---- measurement aid: a kernel that only reads `bytes` bytes (a multiple of 16) once
 hipError_t launch_read_stream(const void* buf, size_t bytes, uint32_t* sink, int blocks, hipStream_t st);
