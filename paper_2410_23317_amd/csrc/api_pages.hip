@@ -64,9 +64,10 @@ vlc_status check_call(const char* who, const vlc_pages* pages, const vlc_chunk* 
     if (c->max_new < 1 || c->max_new > c->max_len || c->max_len > (int64_t)c->max_pages * s.page_slots || c->max_len > 1 << 30)
         return fail(VLC_ERR_SHAPE, "%s: 1 <= max_new = %d <= max_len = %d <= max_pages * page_slots = %lld (and 2^30) does not hold", who,
                     c->max_new, c->max_len, (long long)c->max_pages * s.page_slots);
-    if ((double)c->B * n_layers * s.Hkv * (c->max_len / 1024 + 1) > 1.0e9)
-        return fail(VLC_ERR_SHAPE, "%s: B * layers * Hkv * max_len exceeds 10^12", who);
-    if ((int64_t)c->max_new * s.Hq > 1 << 28) return fail(VLC_ERR_SHAPE, "%s: max_new * Hq = %lld exceeds 2^28", who, (long long)c->max_new * s.Hq);
+    // grids of fewer than 2^24 blocks
+    if ((int64_t)c->B * n_layers * s.Hkv * (c->max_len / 1024 + 1) > 1 << 23 || (int64_t)c->B * n_layers * s.Hq * c->max_new > (int64_t)1 << 30)
+        return fail(VLC_ERR_SHAPE, "%s: B * layers * Hkv * max_len exceeds 2^33, or B * layers * Hq * max_new 2^30", who);
+    if ((int64_t)c->max_new * s.Hq > 1 << 26) return fail(VLC_ERR_SHAPE, "%s: max_new * Hq = %lld exceeds 2^26", who, (long long)c->max_new * s.Hq);
     return VLC_OK;
 }
 
@@ -194,7 +195,7 @@ vlc_status vlc_pages_read(vlc_pages* pages, const vlc_chunk* chunk, int32_t laye
     if (vlc_status st = check_rows(who, "v_out", v_out, s.dtype, true, nl, chunk->B, s.Hkv, count)) return st;
     if (first >= chunk->max_len) return VLC_OK;               // no request holds such a position
     if (count > chunk->max_len - first) count = chunk->max_len - first;
-    if ((int64_t)count * s.Hkv > 1 << 28) return fail(VLC_ERR_SHAPE, "%s: count * Hkv = %lld exceeds 2^28", who, (long long)count * s.Hkv);
+    if ((int64_t)count * s.Hkv > 1 << 26) return fail(VLC_ERR_SHAPE, "%s: count * Hkv = %lld exceeds 2^26", who, (long long)count * s.Hkv);
     const hipError_t e = vlc::launch_pages_read(pages_call(pages, chunk, layer_begin, layer_end, stream), first, count, *k_out, *v_out);
     if (e != hipSuccess) return hip_fail(e, who);
     return VLC_OK;
@@ -207,7 +208,7 @@ vlc_status vlc_pages_attn_workspace_bytes(const vlc_pages* pages, const vlc_chun
     if (vlc_status st = check_layers(who, pages, 0, n_layers)) return st;
     if (vlc_status st = check_call(who, pages, chunk, n_layers)) return st;
     const vlc::PagesCall c = pages_call(pages, chunk, 0, n_layers, nullptr);
-    *bytes_out = vlc::pages_few_supported(c) ? vlc::pages_few_workspace_bytes(c) : 0;
+    *bytes_out = vlc::pages_few_supported(c) ? vlc::pages_few_workspace_bytes(c) : vlc::pages_rows_supported(c) ? vlc::pages_rows_workspace_bytes(c) : 0;
     return VLC_OK;
 }
 
@@ -256,7 +257,7 @@ vlc_status vlc_pages_attn(vlc_pages* pages, const vlc_chunk* chunk, int32_t laye
         const hipError_t e = vlc::launch_pages_write(a.c, *k_new, *v_new);
         if (e != hipSuccess) return hip_fail(e, who);
     }
-    const hipError_t e = vlc::launch_pages_attn_simple(a);
+    const hipError_t e = vlc::pages_rows_supported(a.c) ? vlc::launch_pages_rows(a) : vlc::launch_pages_attn_simple(a);
     if (e != hipSuccess) return hip_fail(e, who);
     return VLC_OK;
 }

@@ -1,0 +1,558 @@
+// Attention of a chunk over the pages of its request (gfx950, v_mfma_f32_32x32x16_bf16): the chunks of a prompt, more than 32
+// query rows per KV head.
+//
+// A block of four waves takes 128 RB query rows of one KV head (rows token after token, the g heads of a token next to each
+// other, so that a block needs few masked keys) and walks the keys.  A wave owns RB blocks of 32 rows.  As in the
+// window attention, S^T = K Q^T per 32 keys, so the 16 logits a lane holds belong to ONE query row, the softmax stays in
+// the lane, the probabilities are the second operand of O^T += V^T P^T as they are, and V's transpose is the LDS read.
+//
+// What decides the speed is that the matrix instructions of one step have something independent to run beside: iteration j
+// turns the logits of keys j into probabilities (vector unit) while the products K Q^T of keys j + 1 run, and then
+// multiplies V of keys j while it takes the maxima of the logits j + 1.  With RB = 2 every fragment read from LDS feeds two
+// matrix instructions: at one, the four waves would need LDS's 128 bytes per clock all the time.
+// The running maximum is raised only when a logit exceeds it by more than 2^kSlack: probabilities are then at most
+// 2^kSlack instead of 1, and the accumulators are rescaled a few times per row instead of at every new maximum.
+//
+// Keys come in stages of 64 through a ring of four LDS buffers: plain rows go from memory to LDS without registers, requested
+// three stages ahead; codes are fetched into registers, expanded to bf16 (exactly) on their way into LDS, and their scales
+// multiply the logits and the probabilities.  16-byte pieces of a row lie at swizzled places, so that neither the reads of K
+// (16 rows, one piece) nor the transposing reads of V (four rows, 64 bytes) meet on a bank.
+#include "pages_attn.h"
+#include "score_tiles.h"
+
+namespace vlc {
+namespace {
+
+using tiles::acc_row;
+
+constexpr int kWaves = 4, kThreads = kWaves * 64;
+constexpr int kStage = 64;             // keys per stage
+constexpr int kRing = 4;
+constexpr float kSlack = 6.f;
+
+struct RowsArgs {
+    PagesAttnParams a;
+    int row_blocks, groups;            // of a KV head's rows; layers * requests * KV heads
+    int stages_per_split;
+    float* part_o;                     // [group][split][rows][D] unnormalised
+    float2* part_mz;                   // [group][split][rows]
+};
+
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
+typedef __attribute__((address_space(3))) void lds_void_t;
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(lds_void_t*)p; }
+
+// 64 lanes x 16 bytes from memory to 1024 contiguous bytes of LDS.  The hardware takes LDS's address from m0.
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const char* base, uint32_t offset) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(offset), "s"(base) : "memory");
+}
+
+// Place of 16-byte piece p of key row r of a stage, in pieces.
+template <int D> __device__ __forceinline__ int k_place(int r, int p) {
+    return r * (D / 8) + (D == 128 ? p ^ (r & 15) : p ^ ((r >> 1) & 7));
+}
+template <int D> __device__ __forceinline__ int v_place(int r, int p) {
+    return r * (D / 8) + (D == 128 ? p ^ ((r & 3) << 2) : p ^ (((r >> 1) & 1) << 2));
+}
+
+__device__ __forceinline__ float max_across_halves(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+template <int D, int FMT, int RB>
+__global__ __launch_bounds__(kThreads, 1) void pages_rows_kernel(RowsArgs ra) {
+    constexpr bool Q8 = PageRow<FMT>::kQuantised;
+    constexpr int KS = D / 16, DT = D / 32, PPR = D / 8;       // k-steps of K Q^T, 32-wide tiles of d, pieces per row
+    constexpr int ROWB = D * PageRow<FMT>::kElemBytes;         // bytes of a row in a page
+    constexpr int LOADS = 2 * kStage * PPR / kThreads;         // 16-byte pieces of K and V per thread and stage (plain rows)
+    __shared__ __align__(1024) uint4 sK[kRing][kStage * PPR];
+    __shared__ __align__(1024) uint4 sV[kRing][kStage * PPR];
+    __shared__ __align__(16) float sKs[Q8 ? kRing : 1][kStage], sVs[Q8 ? kRing : 1][kStage];
+    __shared__ int sBad[2];            // first and last stage in which numbers of V were replaced by 0
+    const PagesAttnParams& a = ra.a;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
+
+    // ---- which rows: the blocks of a KV head on one XCD (the hardware deals consecutive blocks to the 8 XCDs in turn), so that
+    // they share its L2, and the row blocks with the most keys first
+    const int per_group = ra.row_blocks * a.n_units;
+    int group, inner;
+    {
+        const int id = blockIdx.x, x = id & 7;
+        if ((ra.groups & 7) == 0) { group = x + 8 * ((id >> 3) / per_group); inner = (id >> 3) % per_group; }
+        else { group = id % ra.groups; inner = id / ra.groups; }
+    }
+    const int rblk = ra.row_blocks - 1 - inner / a.n_units, split = inner % a.n_units;
+    const int h = group % a.p.Hkv, lb = group / a.p.Hkv, b = lb % a.p.B, l = lb / a.p.B;
+    const ChunkLen len = chunk_len(a.p, b);
+    if (!len.ok && l == 0 && h == 0 && inner == 0 && tid == 0) report_lens(a.p, b);
+    const int g = a.p.g, rows = g * len.c, first_new = len.n - len.c;
+    const int r0 = rblk * (128 * RB);                          // the block's rows: r0 + 32 RB wave + 32 rb + lane % 32
+    if (r0 >= rows) return;
+    const int first_last = first_new + r0 / g;                 // last key of the block's first row, and of its last row
+    const int last_last = first_new + (min(r0 + 128 * RB, rows) - 1) / g;
+    const int st0 = split * ra.stages_per_split, st1 = min(last_last / kStage + 1, st0 + ra.stages_per_split);
+    const int st_masked = (first_last + 1) / kStage;           // first stage that some row does not see to its end
+
+    const float scale = attn_scale(a, l, D), c = tiles::exp_scale(scale);
+    bf16x8_t qf[RB][KS];
+    int last[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        const int r = min(r0 + 32 * (RB * wave + rb) + (lane & 31), rows - 1);         // rows beyond the last repeat it
+        last[rb] = first_new + r / g;
+        const char* q = a.q.at(l, b, h * g + r % g, r / g) + half * 16;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) qf[rb][ks] = *reinterpret_cast<const bf16x8_t*>(q + ks * 32);
+    }
+    // the products stand for the logits only where the scale is positive: Q takes its sign, and is 0 for a scale of 0
+    if (!(scale > 0.f)) {
+        const uint32_t flip = scale < 0.f ? 0x80008000u : 0u, keep = scale == 0.f ? 0u : 0xffffffffu;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                uint4 w = __builtin_bit_cast(uint4, qf[rb][ks]);
+                w = make_uint4((w.x ^ flip) & keep, (w.y ^ flip) & keep, (w.z ^ flip) & keep, (w.w ^ flip) & keep);
+                qf[rb][ks] = __builtin_bit_cast(bf16x8_t, w);
+            }
+    }
+    float m[RB], z[RB], peak[RB];      // what the weights are relative to, their sum, the largest logit; exponent domain
+    f32x16_t o[RB][DT];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        m[rb] = peak[rb] = kNoMax; z[rb] = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[rb][dt] = f32x16_t{0};
+    }
+
+    // ---- stages: page ids of 64 pages in a register, a lane each
+    const int64_t head0 = (int64_t)(a.p.layer_begin + l) * a.p.n_pages * a.p.Hkv + h;
+    const int last_page = (len.n - 1) >> a.p.ps_shift;
+    int id_base = INT32_MIN, ids = 0;
+    auto need_ids = [&](int key0) {
+        const int p0 = key0 >> a.p.ps_shift;
+        if (p0 + ((kStage - 1) >> a.p.ps_shift) < id_base + 64 && id_base >= 0) return;
+        id_base = p0;
+        const int page = p0 + lane;
+        int v = page <= last_page ? a.p.table[(int64_t)b * a.p.max_pages + page] : 0;
+        if ((uint32_t)v >= (uint32_t)a.p.n_pages) {
+            set_sticky(a.p.status, VLC_ERR_INVALID_ARG, b, kStickyPage, v);
+            v = 0;
+        }
+        ids = v;
+    };
+    // first row (of page_slots) of key's page; keys behind the last one of the request are in its last page, or in page 0
+    auto row_of_uniform = [&](int key) {
+        const int v = __builtin_amdgcn_readlane(ids, (key >> a.p.ps_shift) - id_base);
+        return ((head0 + (int64_t)v * a.p.Hkv) << a.p.ps_shift) + (key & ((1 << a.p.ps_shift) - 1));
+    };
+    // plain rows: an instruction of a wave moves 64 / PPR rows
+    constexpr int RPI = 64 / PPR;
+    auto request_plain = [&](int st) {
+        const int key0 = st * kStage;
+        need_ids(key0);
+#pragma unroll
+        for (int u = 0; u < LOADS / 2; ++u) {
+            const int r = (u * kWaves + wave) * RPI;           // first row of the instruction (wave-uniform); its rows share a page
+            const int64_t row = row_of_uniform(key0 + r);
+            const int lr = r + lane / PPR, place = lane % PPR; // the lane's row, and the place in it that it fills
+            const uint32_t kp = k_place<D>(lr, place) % PPR, vp = v_place<D>(lr, place) % PPR;  // (the swizzle is its own inverse)
+            load_to_lds(lds_address(&sK[st & (kRing - 1)][r * PPR]), a.p.k + row * ROWB, (lane / PPR) * ROWB + kp * 16);
+            load_to_lds(lds_address(&sV[st & (kRing - 1)][r * PPR]), a.p.v + row * ROWB, (lane / PPR) * ROWB + vp * 16);
+        }
+    };
+    // codes: a thread fetches 16 at a time
+    constexpr int CPR = D / 16, CODE_LOADS = kStage * CPR / kThreads > 0 ? kStage * CPR / kThreads : 1;
+    uint4 kc[Q8 ? CODE_LOADS : 1], vc[Q8 ? CODE_LOADS : 1];
+    float sc = 0.f;
+    auto row_of_lane = [&](int key) {
+        const int v = __shfl(ids, (key >> a.p.ps_shift) - id_base, kWave);
+        return ((head0 + (int64_t)v * a.p.Hkv) << a.p.ps_shift) + (key & ((1 << a.p.ps_shift) - 1));
+    };
+    auto request_codes = [&](int st) {
+        const int key0 = st * kStage;
+        need_ids(key0);
+#pragma unroll
+        for (int u = 0; u < CODE_LOADS; ++u) {
+            const int x = tid + kThreads * u, r = x / CPR, piece = x % CPR;
+            const int64_t row = row_of_lane(key0 + r);
+            kc[u] = *reinterpret_cast<const uint4*>(a.p.k + row * ROWB + piece * 16);
+            vc[u] = *reinterpret_cast<const uint4*>(a.p.v + row * ROWB + piece * 16);
+        }
+        const int64_t row = row_of_lane(key0 + lane);          // waves 0 and 1: the scales
+        if (wave < 2) sc = (wave ? a.p.v_scale : a.p.k_scale)[row];
+    };
+    auto store_codes = [&](int st) {
+        const int key0 = st * kStage, buf = st & (kRing - 1);
+#pragma unroll
+        for (int u = 0; u < CODE_LOADS; ++u) {
+            const int x = tid + kThreads * u, r = x / CPR, piece = x % CPR;
+            const bool there = key0 + r < len.n;               // stale codes may stand for NaN
+            const uint4 v = there ? vc[u] : make_uint4(0, 0, 0, 0);
+            sK[buf][k_place<D>(r, 2 * piece)] = codes_to_bf16<FMT>(make_uint2(kc[u].x, kc[u].y));
+            sK[buf][k_place<D>(r, 2 * piece + 1)] = codes_to_bf16<FMT>(make_uint2(kc[u].z, kc[u].w));
+            sV[buf][v_place<D>(r, 2 * piece)] = codes_to_bf16<FMT>(make_uint2(v.x, v.y));
+            sV[buf][v_place<D>(r, 2 * piece + 1)] = codes_to_bf16<FMT>(make_uint2(v.z, v.w));
+        }
+        if (wave < 2) (wave ? sVs : sKs)[buf][lane] = wave ? sc : sc * c;
+    };
+
+    auto barrier = [&]() {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    // V of a stage that some row does not see to its end: numbers that are not finite become 0 (0 times them is no 0)
+    auto clean_v = [&](int st) {
+        if constexpr (!Q8) {
+            bool bad = false;
+#pragma unroll
+            for (int u = 0; u < LOADS / 2; ++u) {
+                uint4& w = sV[st & (kRing - 1)][tid + kThreads * u];
+                const uint4 x = w, f = make_uint4(finite_pair(x.x), finite_pair(x.y), finite_pair(x.z), finite_pair(x.w));
+                if (x.x != f.x || x.y != f.y || x.z != f.z || x.w != f.w) { w = f; bad = true; }
+            }
+            if (bad) { atomicMin(&sBad[0], st); atomicMax(&sBad[1], st); }
+            barrier();
+        }
+    };
+
+    // LDS places of the lane's fragments in step 0 of the ring; step j (32 keys) lies (j mod 2 kRing) kStep bytes behind
+    constexpr int kStep = 32 * PPR * 16;
+    uint32_t k_at[KS], v_at[DT];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) k_at[ks] = lds_address(&sK[0][k_place<D>(lane & 31, 2 * ks + half)]);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+        // lane (l % 32) owns row 32 dt + l % 32 of V^T, lane half l / 32 keys 16 sp + 4 half + {0..3, 8..11}: the order of the
+        // accumulators.  ds_read_b64_tr_b16: lane 4 i + e of 16 names 4 numbers of key i, lane x is given number x of the 4 keys
+        const int key = 4 * half + ((lane >> 2) & 3), el = dt * 32 + (lane & 16) + (lane & 3) * 4;
+        v_at[dt] = lds_address(&sV[0][v_place<D>(key, el >> 3)]) + (el & 4) * 2;
+    }
+    auto step_offset = [&](int j) { return (uint32_t)((j & (2 * kRing - 1)) * kStep); };
+    typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+    typedef const __attribute__((address_space(3))) u32x4_t* LdsPieces;
+    auto products = [&](int j, f32x16_t (&acc)[RB]) {                  // logits of the keys of step j
+        const uint32_t off = step_offset(j);
+        bf16x8_t kf[KS];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) kf[ks] = __builtin_bit_cast(bf16x8_t, *(LdsPieces)(k_at[ks] + off));
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) acc[rb] = f32x16_t{0};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) acc[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[rb][ks], acc[rb], 0, 0, 0);
+    };
+    auto scales_of = [&](const float* stage0, int j, float (&f)[16]) { // of the keys whose logits the lane holds
+        const float* at = stage0 + (j & (2 * kRing - 1)) * 32 + 4 * half;
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+            const float4 x = *reinterpret_cast<const float4*>(at + 8 * q4);
+            f[4 * q4] = x.x; f[4 * q4 + 1] = x.y; f[4 * q4 + 2] = x.z; f[4 * q4 + 3] = x.w;
+        }
+    };
+    // Codes: the logits in the exponent domain.  Masked: keys that a row does not see.  Returns whether a running maximum has to
+    // be raised.
+    float top[RB];                     // largest logit of the step, exponent domain
+    auto finish_logits = [&](auto masked, int j, f32x16_t (&acc)[RB]) {
+        constexpr bool MASKED = decltype(masked)::value;
+        float f[16];
+        if constexpr (Q8) scales_of(&sKs[0][0], j, f);
+        bool raise = false;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                if constexpr (Q8) acc[rb][i] *= f[i];
+                if constexpr (MASKED) acc[rb][i] = 32 * j + acc_row(i, lane) <= last[rb] ? acc[rb][i] : -INFINITY;
+            }
+            float t = acc[rb][0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) t = fmaxf(t, acc[rb][i]);
+            top[rb] = Q8 ? t : t * c;
+            peak[rb] = fmaxf(peak[rb], top[rb]);
+            raise |= top[rb] > m[rb] + kSlack;
+        }
+        return __any(raise) != 0;
+    };
+    auto raise_max = [&]() {
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            const float m_new = fmaxf(m[rb], max_across_halves(top[rb])), corr = exp2_fast(m[rb] - m_new);
+            m[rb] = m_new;
+            z[rb] *= corr;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) o[rb][dt] *= corr;
+        }
+    };
+    // Step j, whose logits are in s: its probabilities beside the products of step j + 1 (into sn), its outputs beside the maxima of those.
+    auto step = [&](auto masked, auto final, int j, f32x16_t (&s)[RB], f32x16_t (&sn)[RB]) {
+        constexpr bool MASKED = decltype(masked)::value, LAST = decltype(final)::value;
+        if constexpr (!LAST) products(j + 1, sn);
+        bf16x8_t pf[RB][2];
+        float f[16];
+        if constexpr (Q8) scales_of(&sVs[0][0], j, f);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            float zs = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float p = exp2_fast(Q8 ? s[rb][i] - m[rb] : fmaf(s[rb][i], c, -m[rb]));
+                zs += p;
+                float w = p;
+                if constexpr (Q8) {
+                    w = p * f[i];
+                    if constexpr (MASKED) w = 32 * j + acc_row(i, lane) <= last[rb] ? w : 0.f;        // any scale there
+                }
+                pf[rb][i >> 3][i & 7] = (__bf16)w;
+            }
+            z[rb] += zs;
+        }
+        const uint32_t off = step_offset(j);
+#pragma unroll
+        for (int sp = 0; sp < 2; ++sp)
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                const lds_s16x4_t* at = (const lds_s16x4_t*)(v_at[dt] + off);          // rows of PPR 16-byte pieces
+                const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(at + 16 * sp * PPR * 2));
+                const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(at + (16 * sp + 8) * PPR * 2));
+                const uint2 x = __builtin_bit_cast(uint2, lo), y = __builtin_bit_cast(uint2, hi);
+                const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, make_uint4(x.x, x.y, y.x, y.y));
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) o[rb][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[rb][sp], o[rb][dt], 0, 0, 0);
+            }
+        if constexpr (!LAST) return finish_logits(masked, j + 1, sn);
+        return false;
+    };
+    auto boundary = [&](int st) {      // makes stage st + 1 visible, requests another
+        if constexpr (!Q8) {
+            if (st + 2 < st1) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(LOADS) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            barrier();
+            if (st + 3 < st1) request_plain(st + 3);
+        } else {
+            if (st + 2 < st1) store_codes(st + 2);
+            barrier();
+            if (st + 3 < st1) request_codes(st + 3);
+        }
+    };
+
+    if (tid < 2) sBad[tid] = tid ? -1 : INT32_MAX;
+    if (st0 < st1) {
+        if constexpr (!Q8) {
+            request_plain(st0);
+            if (st0 + 1 < st1) request_plain(st0 + 1);
+            if (st0 + 2 < st1) request_plain(st0 + 2);
+            if (st0 + 2 < st1) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * LOADS) : "memory");
+            else if (st0 + 1 < st1) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(LOADS) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        } else {
+            request_codes(st0);
+            store_codes(st0);
+            if (st0 + 1 < st1) { request_codes(st0 + 1); store_codes(st0 + 1); }
+            if (st0 + 2 < st1) request_codes(st0 + 2);
+        }
+        barrier();
+        if (st0 >= st_masked) clean_v(st0);
+        constexpr auto yes = std::true_type{};
+        constexpr auto no = std::false_type{};
+        f32x16_t s0[RB], s1[RB];
+        int j = 2 * st0;
+        products(j, s0);
+        if (finish_logits(yes, j, s0)) raise_max();
+        // Steps up to jstop.  Raising the maximum stands outside the loop over the steps: inside, the accumulators would have two
+        // definitions to choose from, and be copied at every step.
+        auto run = [&](auto masked, int jstop) {
+            auto one = [&](f32x16_t (&s)[RB], f32x16_t (&sn)[RB]) {
+                if (j & 1) {
+                    boundary(j >> 1);
+                    if constexpr (decltype(masked)::value)
+                        if ((j >> 1) + 1 >= st_masked) clean_v((j >> 1) + 1);
+                }
+                const bool raise = step(masked, no, j, s, sn);
+                ++j;
+                return raise;
+            };
+            while (j < jstop) {
+                bool raise;
+                for (;;) {
+                    raise = one(s0, s1);
+                    if (raise || j >= jstop) {
+#pragma unroll
+                        for (int rb = 0; rb < RB; ++rb) s0[rb] = s1[rb];
+                        break;
+                    }
+                    raise = one(s1, s0);
+                    if (raise || j >= jstop) break;
+                }
+                if (raise) raise_max();
+            }
+        };
+        run(no, min(2 * st1, 2 * st_masked) - 1);               // these steps and the next one are seen by all rows
+        run(yes, 2 * st1 - 1);
+        step(yes, yes, j, s0, s1);
+    }
+    barrier();
+    const int64_t prow0 = ((int64_t)group * a.n_units + split) * ((int64_t)g * a.p.max_new);
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        const int r = r0 + 32 * (RB * wave + rb) + (lane & 31);
+        const float top_m = max_across_halves(peak[rb]), to_top = exp2_fast(m[rb] - top_m);    // relative to the largest logit from here on
+        const float zt = (z[rb] + __shfl_xor(z[rb], 32, kWave)) * to_top;
+        if (r >= rows) continue;
+        if (a.n_units == 1) {
+            const float inv = zt == 0.f ? 0.f : to_top / zt;
+            bf16_t* out = (bf16_t*)a.out.at(l, b, h * g + r % g, r / g);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4) {
+                    bf16_t* dst = out + dt * 32 + acc_row(4 * q4, lane);
+                    store_pair(dst, o[rb][dt][4 * q4] * inv, o[rb][dt][4 * q4 + 1] * inv);
+                    store_pair(dst + 2, o[rb][dt][4 * q4 + 2] * inv, o[rb][dt][4 * q4 + 3] * inv);
+                }
+            if (half == 0 && a.stats.row_max) store_stats(a, l, b, h * g + r % g, r / g, top_m, zt);
+        } else {
+            float* dst = ra.part_o + (prow0 + r) * D;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4)
+                    *reinterpret_cast<float4*>(dst + dt * 32 + acc_row(4 * q4, lane)) =
+                        make_float4(o[rb][dt][4 * q4] * to_top, o[rb][dt][4 * q4 + 1] * to_top, o[rb][dt][4 * q4 + 2] * to_top, o[rb][dt][4 * q4 + 3] * to_top);
+            if (half == 0) ra.part_mz[prow0 + r] = make_float2(top_m, zt);
+        }
+    }
+    // What is not finite in V reaches the rows that see it: added to what was just stored, from memory, a number at a time.
+    if (!Q8 && sBad[0] < st1) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        const int t0 = sBad[0] * kStage, t1 = sBad[1] * kStage + kStage - 1;
+        for (int x = tid; x < min(128 * RB, rows - r0) * D; x += kThreads) {
+            const int r = r0 + x / D, d = x % D;
+            float add = 0.f;
+            bool any = false;
+            for (int t = t0; t <= min(first_new + r / g, t1); ++t) {
+                int page = a.p.table[(int64_t)b * a.p.max_pages + (t >> a.p.ps_shift)];
+                if ((uint32_t)page >= (uint32_t)a.p.n_pages) page = 0;
+                const float f = Elem<bf16_t>::load((const bf16_t*)a.p.v + (page_row0(a.p, a.p.layer_begin + l, page, h) + (t & ((1 << a.p.ps_shift) - 1))) * D + d);
+                if (!is_finite(f)) { add += f; any = true; }
+            }
+            if (!any) continue;
+            if (a.n_units == 1) {
+                bf16_t* out = (bf16_t*)a.out.at(l, b, h * g + r % g, r / g) + d;
+                *reinterpret_cast<__bf16*>(out) = (__bf16)(Elem<bf16_t>::load(out) + add);
+            } else {
+                ra.part_o[(prow0 + r) * D + d] += add;
+            }
+        }
+    }
+}
+
+// Merge of the key splits: D / 4 lanes per row.  A split beyond what the row's block saw has left nothing: kNoMax and 0 are
+// written by its block all the same.
+template <int D>
+__global__ __launch_bounds__(256) void pages_rows_merge_kernel(RowsArgs ra) {
+    const PagesAttnParams& a = ra.a;
+    constexpr int LPR = D / 4;
+    const int sub = threadIdx.x % LPR;
+    const int group = blockIdx.y, h = group % a.p.Hkv, lb = group / a.p.Hkv, b = lb % a.p.B, l = lb / a.p.B;
+    const int r = blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+    const int g = a.p.g;
+    if (r >= g * chunk_len(a.p, b).c) return;
+    const int64_t stride = (int64_t)g * a.p.max_new, p0 = (int64_t)group * a.n_units * stride + r;
+    float m = kNoMax, z = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    constexpr int NB = 4;
+    for (int s0 = 0; s0 < a.n_units; s0 += NB) {
+        float2 mz[NB];
+        float4 f[NB];
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const int64_t at = p0 + min(s0 + j, a.n_units - 1) * stride;
+            mz[j] = ra.part_mz[at];
+            f[j] = *reinterpret_cast<const float4*>(ra.part_o + at * D + sub * 4);
+        }
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+            if (s0 + j < a.n_units) {
+                const float mn = fmaxf(m, mz[j].x), w0 = exp2_fast(m - mn), w1 = exp2_fast(mz[j].x - mn);
+                z = z * w0 + mz[j].y * w1;
+                o.x = o.x * w0 + f[j].x * w1; o.y = o.y * w0 + f[j].y * w1; o.z = o.z * w0 + f[j].z * w1; o.w = o.w * w0 + f[j].w * w1;
+                m = mn;
+            }
+    }
+    const float inv = z == 0.f ? 0.f : 1.f / z;
+    bf16_t* out = (bf16_t*)a.out.at(l, b, h * g + r % g, r / g) + sub * 4;
+    store_pair(out, o.x * inv, o.y * inv);
+    store_pair(out + 2, o.z * inv, o.w * inv);
+    if (sub == 0 && a.stats.row_max) store_stats(a, l, b, h * g + r % g, r / g, m, z);
+}
+
+struct RowsPlan { int rb, row_blocks, splits, stages_per_split; int64_t groups, rows; size_t o_bytes, bytes; };
+
+RowsPlan plan(const PagesCall& c) {
+    RowsPlan p;
+    const int g = c.s.Hq / c.s.Hkv;
+    p.groups = (int64_t)c.n_layers * c.chunk.B * c.s.Hkv;
+    p.rows = (int64_t)g * c.chunk.max_new;
+    p.rb = p.rows <= 128 ? 1 : 2;
+    p.row_blocks = (int)((p.rows + 128 * p.rb - 1) / (128 * p.rb));
+    const int stages = (c.chunk.max_len + kStage - 1) / kStage;
+    const int64_t blocks = p.groups * p.row_blocks;
+    // A block fills a compute unit; a launch takes as many rounds as it has blocks per 256.  Splitting the keys fills the last
+    // round, for a start and an end of about four stages per block and the way of the partial results through memory.
+    int best = 1;
+    double least = 1e300;
+    for (int ns = 1; ns <= 64 && ns * 4 <= stages + 3 && (ns == 1 || blocks * ns <= 8192); ++ns) {
+        const int per = (stages + ns - 1) / ns;
+        double cost = (double)((blocks * ns + 255) / 256) * (per + 4);
+        if (ns > 1) cost += 4 + (double)p.groups * p.rows * ns * c.s.d * 8 / 4.0e6;
+        if (cost < least) { least = cost; best = ns; }
+    }
+    p.stages_per_split = (stages + best - 1) / best;
+    p.splits = (stages + p.stages_per_split - 1) / p.stages_per_split;
+    const size_t n = (size_t)p.groups * p.splits * p.rows;
+    p.o_bytes = (n * c.s.d * sizeof(float) + 255) / 256 * 256;
+    p.bytes = p.splits > 1 ? p.o_bytes + n * sizeof(float2) : 0;
+    return p;
+}
+
+template <int D, int FMT>
+void launch(const RowsArgs& ra, int rb, hipStream_t st) {
+    const unsigned grid = (unsigned)ra.groups * ra.row_blocks * ra.a.n_units;
+    if (rb == 1) pages_rows_kernel<D, FMT, 1><<<grid, kThreads, 0, st>>>(ra);
+    else pages_rows_kernel<D, FMT, 2><<<grid, kThreads, 0, st>>>(ra);
+    if (ra.a.n_units > 1) {
+        constexpr int per = 256 / (D / 4);
+        pages_rows_merge_kernel<D><<<dim3((ra.a.p.g * ra.a.p.max_new + per - 1) / per, ra.groups), 256, 0, st>>>(ra);
+    }
+}
+
+}  // namespace
+
+bool pages_rows_supported(const PagesCall& c) { return c.s.dtype == VLC_BF16; }
+size_t pages_rows_workspace_bytes(const PagesCall& c) { return plan(c).bytes; }
+
+hipError_t launch_pages_rows(const PagesAttn& c) {
+    const RowsPlan p = plan(c.c);
+    RowsArgs ra;
+    ra.a = pages_attn_params(c);
+    ra.a.n_units = p.splits;
+    ra.row_blocks = p.row_blocks; ra.groups = (int)p.groups; ra.stages_per_split = p.stages_per_split;
+    ra.part_o = (float*)c.workspace;
+    ra.part_mz = (float2*)((char*)c.workspace + p.o_bytes);
+    const bool wide = c.c.s.d == 128;
+    switch (page_format(c.c.s)) {
+        case kPageBf16: wide ? launch<128, kPageBf16>(ra, p.rb, c.c.stream) : launch<64, kPageBf16>(ra, p.rb, c.c.stream); break;
+        case kPageFp8: wide ? launch<128, kPageFp8>(ra, p.rb, c.c.stream) : launch<64, kPageFp8>(ra, p.rb, c.c.stream); break;
+        case kPageInt8: wide ? launch<128, kPageInt8>(ra, p.rb, c.c.stream) : launch<64, kPageInt8>(ra, p.rb, c.c.stream); break;
+        case kPageF32: break;
+    }
+    return hipGetLastError();
+}
+
+}  // namespace vlc
