@@ -208,7 +208,9 @@ vlc_status vlc_pages_attn_workspace_bytes(const vlc_pages* pages, const vlc_chun
     if (vlc_status st = check_layers(who, pages, 0, n_layers)) return st;
     if (vlc_status st = check_call(who, pages, chunk, n_layers)) return st;
     const vlc::PagesCall c = pages_call(pages, chunk, 0, n_layers, nullptr);
-    *bytes_out = vlc::pages_few_supported(c) ? vlc::pages_few_workspace_bytes(c) : vlc::pages_rows_supported(c) ? vlc::pages_rows_workspace_bytes(c) : 0;
+    *bytes_out = vlc::pages_few_supported(c) ? vlc::pages_few_workspace_bytes(c)
+                 : c.s.dtype == VLC_F32        ? vlc::pages_rows_f32_workspace_bytes(c)
+                                               : vlc::pages_rows_workspace_bytes(c);
     return VLC_OK;
 }
 
@@ -257,7 +259,7 @@ vlc_status vlc_pages_attn(vlc_pages* pages, const vlc_chunk* chunk, int32_t laye
         const hipError_t e = vlc::launch_pages_write(a.c, *k_new, *v_new);
         if (e != hipSuccess) return hip_fail(e, who);
     }
-    const hipError_t e = vlc::pages_rows_supported(a.c) ? vlc::launch_pages_rows(a) : vlc::launch_pages_attn_simple(a);
+    const hipError_t e = a.c.s.dtype == VLC_F32 ? vlc::launch_pages_rows_f32(a) : vlc::launch_pages_rows(a);
     if (e != hipSuccess) return hip_fail(e, who);
     return VLC_OK;
 }

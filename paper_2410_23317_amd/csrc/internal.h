@@ -211,15 +211,15 @@ struct PagesAttn {
     vlc_row_stats stats;               // row_max null: none
     void* workspace;
 };
-hipError_t launch_pages_attn_simple(const PagesAttn& a);
 // at most 32 query rows per KV head (pages_attn_few.hip); writes the chunk's rows itself
 bool pages_few_supported(const PagesCall& c);
 size_t pages_few_workspace_bytes(const PagesCall& c);
 hipError_t launch_pages_few(const PagesAttn& a);
-// bf16 storage, any number of rows (pages_attn_rows.hip); the chunk's rows are in the pages
-bool pages_rows_supported(const PagesCall& c);
+// any number of rows, which are in the pages: bf16 storage (pages_attn_rows.hip), fp32 storage (pages_attn_rows_f32.hip)
 size_t pages_rows_workspace_bytes(const PagesCall& c);
 hipError_t launch_pages_rows(const PagesAttn& a);
+size_t pages_rows_f32_workspace_bytes(const PagesCall& c);
+hipError_t launch_pages_rows_f32(const PagesAttn& a);
 
 // ---- measurement aid: a kernel that only reads `bytes` bytes (a multiple of 16) once
 hipError_t launch_read_stream(const void* buf, size_t bytes, uint32_t* sink, int blocks, hipStream_t st);

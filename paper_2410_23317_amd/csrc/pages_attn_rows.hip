@@ -534,7 +534,6 @@ void launch(const RowsArgs& ra, int rb, hipStream_t st) {
 
 }  // namespace
 
-bool pages_rows_supported(const PagesCall& c) { return c.s.dtype == VLC_BF16; }
 size_t pages_rows_workspace_bytes(const PagesCall& c) { return plan(c).bytes; }
 
 hipError_t launch_pages_rows(const PagesAttn& c) {
