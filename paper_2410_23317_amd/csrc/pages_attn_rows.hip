@@ -28,7 +28,7 @@ using tiles::acc_row;
 constexpr int kWaves = 4, kThreads = kWaves * 64;
 constexpr int kStage = 64;             // keys per stage
 constexpr int kRing = 4;
-constexpr float kSlack = 6.f;
+constexpr float kSlack = 10.f;
 
 struct RowsArgs {
     PagesAttnParams a;
@@ -288,9 +288,10 @@ __global__ __launch_bounds__(kThreads, 1) void pages_rows_kernel(RowsArgs ra) {
             for (int dt = 0; dt < DT; ++dt) o[rb][dt] *= corr;
         }
     };
-    // Step j, whose logits are in s: its probabilities beside the products of step j + 1 (into sn), its outputs beside the maxima of those.
-    auto step = [&](auto masked, auto final, int j, f32x16_t (&s)[RB], f32x16_t (&sn)[RB]) {
+    // Step j, whose logits are in s: its probabilities beside the products of step j + 1 (which take their place), its outputs beside the maxima of those.
+    auto step = [&](auto masked, auto final, int j, f32x16_t (&s)[RB]) {
         constexpr bool MASKED = decltype(masked)::value, LAST = decltype(final)::value;
+        f32x16_t sn[RB];
         if constexpr (!LAST) products(j + 1, sn);
         bf16x8_t pf[RB][2];
         float f[16];
@@ -324,8 +325,11 @@ __global__ __launch_bounds__(kThreads, 1) void pages_rows_kernel(RowsArgs ra) {
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb) o[rb][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[rb][sp], o[rb][dt], 0, 0, 0);
             }
-        if constexpr (!LAST) return finish_logits(masked, j + 1, sn);
-        return false;
+        if constexpr (LAST) return false;
+        const bool raise = finish_logits(masked, j + 1, sn);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) s[rb] = sn[rb];
+        return raise;
     };
     auto boundary = [&](int st) {      // makes stage st + 1 visible, requests another
         if constexpr (!Q8) {
@@ -359,41 +363,32 @@ __global__ __launch_bounds__(kThreads, 1) void pages_rows_kernel(RowsArgs ra) {
         if (st0 >= st_masked) clean_v(st0);
         constexpr auto yes = std::true_type{};
         constexpr auto no = std::false_type{};
-        f32x16_t s0[RB], s1[RB];
+        f32x16_t s[RB];
         int j = 2 * st0;
-        products(j, s0);
-        if (finish_logits(yes, j, s0)) raise_max();
+        products(j, s);
+        if (finish_logits(yes, j, s)) raise_max();
         // Steps up to jstop.  Raising the maximum stands outside the loop over the steps: inside, the accumulators would have two
         // definitions to choose from, and be copied at every step.
         auto run = [&](auto masked, int jstop) {
-            auto one = [&](f32x16_t (&s)[RB], f32x16_t (&sn)[RB]) {
-                if (j & 1) {
-                    boundary(j >> 1);
-                    if constexpr (decltype(masked)::value)
-                        if ((j >> 1) + 1 >= st_masked) clean_v((j >> 1) + 1);
-                }
-                const bool raise = step(masked, no, j, s, sn);
-                ++j;
-                return raise;
-            };
+#pragma unroll 1
             while (j < jstop) {
                 bool raise;
-                for (;;) {
-                    raise = one(s0, s1);
-                    if (raise || j >= jstop) {
-#pragma unroll
-                        for (int rb = 0; rb < RB; ++rb) s0[rb] = s1[rb];
-                        break;
+#pragma unroll 1
+                do {
+                    if (j & 1) {
+                        boundary(j >> 1);
+                        if constexpr (decltype(masked)::value)
+                            if ((j >> 1) + 1 >= st_masked) clean_v((j >> 1) + 1);
                     }
-                    raise = one(s1, s0);
-                    if (raise || j >= jstop) break;
-                }
+                    raise = step(masked, no, j, s);
+                    ++j;
+                } while (!raise && j < jstop);
                 if (raise) raise_max();
             }
         };
         run(no, min(2 * st1, 2 * st_masked) - 1);               // these steps and the next one are seen by all rows
         run(yes, 2 * st1 - 1);
-        step(yes, yes, j, s0, s1);
+        step(yes, yes, j, s);
     }
     barrier();
     const int64_t prow0 = ((int64_t)group * a.n_units + split) * ((int64_t)g * a.p.max_new);
