@@ -234,11 +234,13 @@ __global__ __launch_bounds__(kThreads, 1) void pages_rows_kernel(RowsArgs ra) {
     auto step_offset = [&](int j) { return (uint32_t)((j & (2 * kRing - 1)) * kStep); };
     typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
     typedef const __attribute__((address_space(3))) u32x4_t* LdsPieces;
-    auto products = [&](int j, f32x16_t (&acc)[RB]) {                  // logits of the keys of step j
+    bf16x8_t kf[KS];
+    auto load_k = [&](int j) {         // fragments of the keys of step j; behind the last one: of whatever the ring holds there
         const uint32_t off = step_offset(j);
-        bf16x8_t kf[KS];
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) kf[ks] = __builtin_bit_cast(bf16x8_t, *(LdsPieces)(k_at[ks] + off));
+    };
+    auto products = [&](f32x16_t (&acc)[RB]) {                         // logits of the keys in kf
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) acc[rb] = f32x16_t{0};
 #pragma unroll
@@ -292,17 +294,17 @@ __global__ __launch_bounds__(kThreads, 1) void pages_rows_kernel(RowsArgs ra) {
     auto step = [&](auto masked, auto final, int j, f32x16_t (&s)[RB]) {
         constexpr bool MASKED = decltype(masked)::value, LAST = decltype(final)::value;
         f32x16_t sn[RB];
-        if constexpr (!LAST) products(j + 1, sn);
+        if constexpr (!LAST) products(sn);
         bf16x8_t pf[RB][2];
         float f[16];
         if constexpr (Q8) scales_of(&sVs[0][0], j, f);
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-            float zs = 0.f;
+            float zs[2] = {0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const float p = exp2_fast(Q8 ? s[rb][i] - m[rb] : fmaf(s[rb][i], c, -m[rb]));
-                zs += p;
+                zs[i & 1] += p;
                 float w = p;
                 if constexpr (Q8) {
                     w = p * f[i];
@@ -310,8 +312,10 @@ __global__ __launch_bounds__(kThreads, 1) void pages_rows_kernel(RowsArgs ra) {
                 }
                 pf[rb][i >> 3][i & 7] = (__bf16)w;
             }
-            z[rb] += zs;
+            z[rb] += zs[0] + zs[1];
+            asm volatile("" : "+v"(z[rb]));    // here, beside the products, not behind the step
         }
+        if constexpr (!LAST) load_k(j + 2);
         const uint32_t off = step_offset(j);
 #pragma unroll
         for (int sp = 0; sp < 2; ++sp)
@@ -326,6 +330,8 @@ __global__ __launch_bounds__(kThreads, 1) void pages_rows_kernel(RowsArgs ra) {
                 for (int rb = 0; rb < RB; ++rb) o[rb][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[rb][sp], o[rb][dt], 0, 0, 0);
             }
         if constexpr (LAST) return false;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) asm volatile("" : "+v"(sn[rb]));       // out of the accumulation registers once, not for each use
         const bool raise = finish_logits(masked, j + 1, sn);
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) s[rb] = sn[rb];
@@ -365,7 +371,9 @@ __global__ __launch_bounds__(kThreads, 1) void pages_rows_kernel(RowsArgs ra) {
         constexpr auto no = std::false_type{};
         f32x16_t s[RB];
         int j = 2 * st0;
-        products(j, s);
+        load_k(j);
+        products(s);
+        load_k(j + 1);
         if (finish_logits(yes, j, s)) raise_max();
         // Steps up to jstop.  Raising the maximum stands outside the loop over the steps: inside, the accumulators would have two
         // definitions to choose from, and be copied at every step.
@@ -375,7 +383,7 @@ __global__ __launch_bounds__(kThreads, 1) void pages_rows_kernel(RowsArgs ra) {
                 bool raise;
 #pragma unroll 1
                 do {
-                    if (j & 1) {
+                    if (!(j & 1) && (j >> 1) + 1 < st1) {      // a step before the stage's first fragments are read
                         boundary(j >> 1);
                         if constexpr (decltype(masked)::value)
                             if ((j >> 1) + 1 >= st_masked) clean_v((j >> 1) + 1);
@@ -386,7 +394,7 @@ __global__ __launch_bounds__(kThreads, 1) void pages_rows_kernel(RowsArgs ra) {
                 if (raise) raise_max();
             }
         };
-        run(no, min(2 * st1, 2 * st_masked) - 1);               // these steps and the next one are seen by all rows
+        run(no, min(2 * st1, 2 * st_masked) - 2);               // these steps, and what they look ahead to, are seen by all rows
         run(yes, 2 * st1 - 1);
         step(yes, yes, j, s);
     }
