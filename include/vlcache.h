@@ -447,7 +447,7 @@ vlc_status vlc_pages_status(vlc_pages* pages, vlc_stream stream);
  *   lens     DEVICE int32 [B][2] = (n_b, c_b), 0 <= c_b <= max_new, c_b <= n_b <= max_len; or NULL: (max_len, max_new)
  *            for every request.  A request may have no new tokens (c_b = 0), or be empty.
  *   max_new  rows per request in the chunk's tensors; max_len bounds n_b and sizes the launch (a captured graph whose
- *            lens grow from replay to replay takes the largest):  1 <= max_new <= max_len <= max_pages * page_slots
+ *            lens grow from replay to replay takes the largest):  1 <= max_new <= max_len <= max_pages * page_slots, max_len <= 2^25
  * Both arrays are read when a call's kernels run.  A request whose lengths break these bounds is skipped, an entry of the
  * table outside [0, n_pages) is taken as page 0 for reading (that request's results are then meaningless) and not written
  * to; either sets the sticky status to VLC_ERR_INVALID_ARG.  Requests may share pages that no call writes to; two rows

@@ -61,8 +61,8 @@ vlc_status check_call(const char* who, const vlc_pages* pages, const vlc_chunk* 
     if (c->B < 1 || c->max_pages < 1) return fail(VLC_ERR_SHAPE, "%s: B and max_pages must be positive", who);
     if ((int64_t)c->B * n_layers * s.Hkv > 65535)
         return fail(VLC_ERR_SHAPE, "%s: B * layers * Hkv = %lld exceeds 65535", who, (long long)c->B * n_layers * s.Hkv);
-    if (c->max_new < 1 || c->max_new > c->max_len || c->max_len > (int64_t)c->max_pages * s.page_slots || c->max_len > 1 << 30)
-        return fail(VLC_ERR_SHAPE, "%s: 1 <= max_new = %d <= max_len = %d <= max_pages * page_slots = %lld (and 2^30) does not hold", who,
+    if (c->max_new < 1 || c->max_new > c->max_len || c->max_len > (int64_t)c->max_pages * s.page_slots || c->max_len > 1 << 25)
+        return fail(VLC_ERR_SHAPE, "%s: 1 <= max_new = %d <= max_len = %d <= max_pages * page_slots = %lld (and 2^25) does not hold", who,
                     c->max_new, c->max_len, (long long)c->max_pages * s.page_slots);
     // grids of fewer than 2^24 blocks
     if ((int64_t)c->B * n_layers * s.Hkv * (c->max_len / 1024 + 1) > 1 << 23 || (int64_t)c->B * n_layers * s.Hq * c->max_new > (int64_t)1 << 30)

@@ -20,6 +20,7 @@ struct PagesAttnParams {
     int unit_shift;                    // log2 of the positions of a unit (the few-row kernel)
     int n_units;                       // units, or key splits, that a row of max_len positions has
     int part_floats;                   // floats of a unit's partial result
+    int g_inverse;                     // 65536 / g, rounded up: x / g = x g_inverse / 65536 for small x
 };
 
 inline PagesAttnParams pages_attn_params(const PagesAttn& c) {
@@ -31,6 +32,7 @@ inline PagesAttnParams pages_attn_params(const PagesAttn& c) {
     a.stats = c.stats;
     a.partials = (float*)c.workspace;
     a.counters = c.c.dev.counters;
+    a.g_inverse = 65536 / a.p.g + 1;
     return a;
 }
 
@@ -49,9 +51,18 @@ __device__ __forceinline__ void store_agent2(float* p, float a, float b) {
     const unsigned long long v = ((unsigned long long)__float_as_uint(b) << 32) | __float_as_uint(a);
     __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-__device__ __forceinline__ float2 load_agent2(const float* p) {
-    const unsigned long long v = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+// (loads through a buffer resource, with the cache-policy bit that a device-scope atomic load sets: 16 bytes at a time)
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+constexpr int kDeviceScope = 16;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t partials_buffer(const float* base, int bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(base), 0, bytes, 0x00020000);
+}
+__device__ __forceinline__ f32x4_t buffer_load16_agent(__amdgpu_buffer_rsrc_t b, int off) {
+    return __builtin_bit_cast(f32x4_t, (u32x4_t)__builtin_amdgcn_raw_buffer_load_b128(b, off, 0, kDeviceScope));
+}
+__device__ __forceinline__ float2 buffer_load8_agent(__amdgpu_buffer_rsrc_t b, int off) {
+    return __builtin_bit_cast(float2, (u32x2_t)__builtin_amdgcn_raw_buffer_load_b64(b, off, 0, kDeviceScope));
 }
 
 // two neighbouring outputs as one store

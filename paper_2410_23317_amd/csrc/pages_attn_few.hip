@@ -57,6 +57,15 @@ __device__ __forceinline__ float sum_over_groups(float v) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// The new rows of a call that writes them, as the pages hold them: the last tile of a wave takes them from here, so that nothing
+// waits until the stores into the pages can be read back.
+template <int D, int FMT, int ROWS>
+struct NewRows {
+    static constexpr int RB = D * PageRow<FMT>::kElemBytes;
+    uint4 k[ROWS][RB / 16], v[ROWS][RB / 16];
+    float ks[PageRow<FMT>::kQuantised ? ROWS : 1], vs[PageRow<FMT>::kQuantised ? ROWS : 1];
+};
+
 template <int D, int FMT, int NT>
 struct FewTile {                                // bf16 operands
     static constexpr bool Q8 = PageRow<FMT>::kQuantised;
@@ -114,6 +123,28 @@ struct FewTile {                                // bf16 operands
             const float4* sc = reinterpret_cast<const float4*>(r.vs + row);
             const float4 a = sc[0], b = sc[1];
             vsc[0] = a.x; vsc[1] = a.y; vsc[2] = a.z; vsc[3] = a.w; vsc[4] = b.x; vsc[5] = b.y; vsc[6] = b.z; vsc[7] = b.w;
+        }
+    }
+    // New rows (positions first_new on) in place of what was requested for them.
+    template <int ROWS>
+    __device__ __forceinline__ void take_new(const NewRows<D, FMT, ROWS>& n, int first_new, int len, int t0, int lane) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int i = t0 + 8 * ((lane >> 2) & 3) + (lane & 3) + 4 * t - first_new;
+            if (i >= 0 && i < len - first_new) {
+#pragma unroll
+                for (int s = 0; s < KLD; ++s) kf[t][s] = *reinterpret_cast<const uint4*>((const char*)n.k[i] + (lane >> 4) * 16 + 64 * s);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = t0 + 8 * (lane >> 4) + j - first_new;
+            if (i >= 0 && i < len - first_new) {
+                const uint32_t* p = reinterpret_cast<const uint32_t*>((const char*)n.v[i] + (lane & 15) * (RB / 16));
+#pragma unroll
+                for (int w = 0; w < VW; ++w) vw[j][w] = p[w];
+                if constexpr (Q8) { ksc[j] = n.ks[i]; vsc[j] = n.vs[i]; }
+            }
         }
     }
     template <bool MASKED>
@@ -202,7 +233,6 @@ struct FewTile {                                // bf16 operands
                 if constexpr (VW == 2) { v[j][2] = b.z; v[j][3] = b.w; }
             }
         }
-        typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 #pragma unroll
         for (int e = 0; e < EV; ++e) {
             u32x4_t vt;
@@ -245,6 +275,22 @@ struct FewTile<D, kPageF32, NT> {               // fp32 operands
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int h = 0; h < VP; ++h) vf[j][h] = *reinterpret_cast<const f32x4_t*>(p + j * RB + 256 * h);
+    }
+    template <int ROWS>
+    __device__ __forceinline__ void take_new(const NewRows<D, kPageF32, ROWS>& n, int first_new, int len, int t0, int lane) {
+        const int i = t0 + (lane & 15) - first_new;
+        if (i >= 0 && i < len - first_new) {
+#pragma unroll
+            for (int s = 0; s < KP; ++s) kf[s] = *reinterpret_cast<const f32x4_t*>((const char*)n.k[i] + (lane >> 4) * 16 + 64 * s);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = t0 + 4 * (lane >> 4) + j - first_new;
+            if (i >= 0 && i < len - first_new) {
+#pragma unroll
+                for (int h = 0; h < VP; ++h) vf[j][h] = *reinterpret_cast<const f32x4_t*>((const char*)n.v[i] + (lane & 15) * 16 + 256 * h);
+            }
+        }
     }
     template <bool MASKED>
     __device__ __forceinline__ void logits(const Columns<NT>& col, float scale2, int t0, int lane) {
@@ -311,44 +357,68 @@ struct FewTile<D, kPageF32, NT> {               // fp32 operands
     }
 };
 
-// The unit's new rows into their pages, by the whole block; ids: the page ids as r.ids, -1 for a page that is none.
-template <int D, int FMT>
-__device__ __forceinline__ void write_new_rows(const PagesAttnParams& a, const CacheRow& r, int l, int b, int h, int from, int to, int first_new, int ids) {
+// Rows first_new + i, i in [from, to), into LDS and into their pages, by the whole block; ids: the page ids as r.ids, -1 for
+// a page that is none and is not written to.
+template <int D, int FMT, int ROWS>
+__device__ __forceinline__ void write_new_rows(const PagesAttnParams& a, const CacheRow& r, NewRows<D, FMT, ROWS>& n, int l, int b, int h, int from, int to,
+                                               int first_new, int ids) {
     typedef PageRow<FMT> R;
     typedef typename R::T T;
     constexpr int LPR = D * (int)sizeof(T) / 16;
     const int sub = threadIdx.x % LPR;
-    for (int t0 = from; t0 < to; t0 += kThreads / LPR) {        // block-uniform: row_of is a wave's
-        const int t = t0 + threadIdx.x / LPR;
-        const int64_t row = r.row_of(min(t, to - 1));
-        const int id = __shfl(ids, (min(t, to - 1) >> r.ps_shift) - r.first_page, kWave);
-        if (t >= to || id < 0) continue;                        // a page that is none is not written to
-        const uint4 kx = reinterpret_cast<const uint4*>(a.k_new.at(l, b, h, t - first_new))[sub];
-        const uint4 vx = reinterpret_cast<const uint4*>(a.v_new.at(l, b, h, t - first_new))[sub];
+    for (int i0 = from; i0 < to; i0 += kThreads / LPR) {        // block-uniform: row_of is a wave's
+        const int i = min(i0 + (int)threadIdx.x / LPR, to - 1), t = first_new + i;
+        const int64_t row = r.row_of(t);
+        const bool there = __shfl(ids, (t >> r.ps_shift) - r.first_page, kWave) >= 0;
+        if (i0 + (int)threadIdx.x / LPR >= to) break;
+        const uint4 kx = reinterpret_cast<const uint4*>(a.k_new.at(l, b, h, i))[sub];
+        const uint4 vx = reinterpret_cast<const uint4*>(a.v_new.at(l, b, h, i))[sub];
         if constexpr (!R::kQuantised) {
-            reinterpret_cast<uint4*>(a.p.k)[row * LPR + sub] = kx;
-            reinterpret_cast<uint4*>(a.p.v)[row * LPR + sub] = vx;
+            n.k[i][sub] = kx;
+            n.v[i][sub] = vx;
+            if (there) {
+                reinterpret_cast<uint4*>(a.p.k)[row * LPR + sub] = kx;
+                reinterpret_cast<uint4*>(a.p.v)[row * LPR + sub] = vx;
+            }
         } else {
             float ks, vs;
             const uint2 kc = quantize_page_row<FMT, LPR>(kx, ks), vc = quantize_page_row<FMT, LPR>(vx, vs);
-            reinterpret_cast<uint2*>(a.p.k)[row * LPR + sub] = kc;
-            reinterpret_cast<uint2*>(a.p.v)[row * LPR + sub] = vc;
-            if (sub == 0) { a.p.k_scale[row] = ks; a.p.v_scale[row] = vs; }
+            reinterpret_cast<uint2*>(n.k[i])[sub] = kc;
+            reinterpret_cast<uint2*>(n.v[i])[sub] = vc;
+            if (sub == 0) { n.ks[i] = ks; n.vs[i] = vs; }
+            if (there) {
+                reinterpret_cast<uint2*>(a.p.k)[row * LPR + sub] = kc;
+                reinterpret_cast<uint2*>(a.p.v)[row * LPR + sub] = vc;
+                if (sub == 0) { a.p.k_scale[row] = ks; a.p.v_scale[row] = vs; }
+            }
         }
     }
 }
 
+// Outputs e .. e + 3 of column c, and its statistics.
+template <typename T>
+__device__ __forceinline__ void store_column(const PagesAttnParams& a, int l, int b, int h, int c, int e, const f32x4_t& o, float m, float z) {
+    const int head = h * a.p.g + c % a.p.g, i = c / a.p.g;
+    T* out = (T*)a.out.at(l, b, head, i) + e;
+    const float div = z == 0.f ? 1.f : z;                       // a row without weights: its sums are 0
+    store_pair(out, o[0] / div, o[1] / div);
+    store_pair(out + 2, o[2] / div, o[3] / div);
+    if (e == 0 && a.stats.row_max) store_stats(a, l, b, head, i, m, z);
+}
+
 template <int D, int FMT, int NT>
-__global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void pages_few_kernel(PagesAttnParams a) {
+__global__ __launch_bounds__(kThreads, NT == 1 ? 3 : NT == 2 ? 2 : 1) void pages_few_kernel(PagesAttnParams a) {
+    constexpr bool ONE_LAUNCH = NT == 1;        // the last unit of a row merges; else a second kernel does
     typedef typename PageRow<FMT>::T T;
     typedef FewTile<D, FMT, NT> Tile;
     constexpr int TK = Tile::TK, STEP = kWaves * TK, DL = D + 4;
+    static_assert(16 * NT <= STEP - TK, "the new tokens lie in the waves' last tiles");
     __shared__ __align__(16) float sMerge[kWaves][16][DL];
+    __shared__ NewRows<D, FMT, 16 * NT> sNew;
     __shared__ int sLast, sNotFinite[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-    const int rows = a.p.n_layers * a.p.B * a.p.Hkv;
-    const int row = blockIdx.x % rows, unit = blockIdx.x / rows;    // the first units of all rows come first
-    const int h = row % a.p.Hkv, lb = row / a.p.Hkv, b = lb % a.p.B, l = lb / a.p.B;
+    const int h = blockIdx.x, lb = blockIdx.y, unit = blockIdx.z;   // the first units of all rows come first, those that may be empty last
+    const int b = lb % a.p.B, l = lb / a.p.B, row = lb * a.p.Hkv + h;
     CacheRow r;
     r.k = a.p.k; r.v = a.p.v; r.ks = a.p.k_scale; r.vs = a.p.v_scale;
     r.Hkv = a.p.Hkv; r.ps_shift = a.p.ps_shift;
@@ -368,19 +438,15 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void pages_few_kernel(Pa
     if (bad_id && wave == 0) set_sticky(a.p.status, VLC_ERR_INVALID_ARG, b, kStickyPage, id);
     r.ids = held && !bad_id ? id : 0;
     const int g = a.p.g, cols = g * len.c, first_new = len.n - len.c;
-    if (a.k_new.data && end > first_new) {
-        write_new_rows<D, FMT>(a, r, l, b, h, max(begin, first_new), end, first_new, bad_id ? -1 : r.ids);
-        __threadfence_block();
-        __syncthreads();
-    }
     Columns<NT> col;
     col.len = len.n;
     Tile tile;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const int c = min(16 * nt + (lane & 15), cols - 1);         // columns beyond the last repeat it; their results are not kept
-        col.last[nt] = first_new + c / g;
-        tile.begin(nt, (const T*)a.q.at(l, b, h * g + c % g, c / g), lane);
+        const int i = (c * a.g_inverse) >> 16;                      // c / g: c < 64
+        col.last[nt] = first_new + i;
+        tile.begin(nt, (const T*)a.q.at(l, b, h * g + c - i * g, i), lane);
     }
     const float scale2 = attn_scale(a, l, D) * kLog2e;
 
@@ -388,11 +454,18 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void pages_few_kernel(Pa
     // Positions behind the last one are read too (slots of the same page, or of page 0 in place of a page that is not there).
     // K of the next tile is requested as soon as the logits are formed, V as soon as the outputs are: the same registers.
     int t0 = begin + wave * TK;
+    const bool fresh = a.k_new.data && end > first_new;         // block-uniform
     if (t0 < end) {
         tile.request_k(r, t0, lane);
         tile.request_v(r, t0, lane);
-        // Only the last tile of a wave can reach beyond what every column sees: at most 32 new tokens stand at the row's end,
-        // and the tiles before a wave's last one end STEP - TK >= 48 positions earlier.
+    }
+    if (fresh) {
+        write_new_rows<D, FMT>(a, r, sNew, l, b, h, max(begin - first_new, 0), end - first_new, first_new, bad_id ? -1 : r.ids);
+        __syncthreads();
+    }
+    if (t0 < end) {
+        // Only the last tile of a wave can reach beyond what every column sees: the at most 16 NT new tokens stand at the
+        // row's end, and the tiles before a wave's last one end STEP - TK = 96 (fp32: 48) positions before the unit does.
 #pragma unroll 1
         for (; t0 + STEP < end; t0 += STEP) {
             tile.template logits<false>(col, scale2, t0, lane);
@@ -400,8 +473,9 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void pages_few_kernel(Pa
             tile.template outputs<false>(col, t0, lane);
             tile.request_v(r, t0 + STEP, lane);
         }
+        if (fresh) tile.take_new(sNew, first_new, end, t0, lane);
         tile.template logits<true>(col, scale2, t0, lane);
-        not_finite = tile.clean_v(col, t0, lane);
+        if (t0 + TK > first_new + 1) not_finite = tile.clean_v(col, t0, lane);
         tile.template outputs<true>(col, t0, lane);
     }
 
@@ -412,17 +486,28 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void pages_few_kernel(Pa
     }
     // What is not finite in V reaches the columns that see it: from memory, a number at a time.  (Codes are finite; a row
     // that was not has a scale of NaN, which the probability takes.)
-    auto add_not_finite = [&](int last, int e, float& o0, float& o1) {
+    auto add_not_finite = [&](int last, int e, f32x4_t& o) {
         if constexpr (!PageRow<FMT>::kQuantised) {
-            for (int t = max(begin, (end - STEP + TK - 1) & -TK); t < min(end, last + 1); ++t) {     // the waves' last tiles
+            for (int t = max(begin, (first_new + 1) & -TK); t < min(end, last + 1); ++t) {       // the tiles that were cleaned
                 int page = a.p.table[(int64_t)b * a.p.max_pages + (t >> a.p.ps_shift)];
                 if ((uint32_t)page >= (uint32_t)a.p.n_pages) page = 0;
                 const T* v = (const T*)a.p.v + (page_row0(a.p, a.p.layer_begin + l, page, h) + (t & ((1 << a.p.ps_shift) - 1))) * D + e;
-                const float f0 = Elem<T>::load(v), f1 = Elem<T>::load(v + 1);
-                if (!is_finite(f0)) o0 += f0;
-                if (!is_finite(f1)) o1 += f1;
+                if (fresh && t >= first_new) v = (const T*)sNew.v[t - first_new] + e;       // its store may still be on its way
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float f = Elem<T>::load(v + i);
+                    if (!is_finite(f)) o[i] += f;
+                }
             }
         }
+    };
+
+    auto store_out = [&](int c, int e, const f32x4_t& o, float m, float z) { store_column<T>(a, l, b, h, c, e, o, m, z); };
+    auto any_not_finite = [&]() {
+        int any = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) any |= sNotFinite[w];
+        return any != 0;
     };
 
     float* part = a.partials + ((int64_t)row * a.n_units + unit) * a.part_floats;
@@ -443,30 +528,33 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void pages_few_kernel(Pa
             if (lane < 16) { dst[D] = tile.m_run[nt]; dst[D + 1] = z; }
         }
         __syncthreads();
-        for (int x = tid; x < nc * (D / 2); x += kThreads) {
-            const int cc = x / (D / 2), e = x % (D / 2) * 2;
-            float m = kNoMax, o0 = 0.f, o1 = 0.f, zz = 0.f;
+        for (int x = tid; x < nc * (D / 4); x += kThreads) {
+            const int cc = x / (D / 4), e = x % (D / 4) * 4;
+            float m = kNoMax, zz = 0.f;
+            f32x4_t o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) m = fmaxf(m, sMerge[w][cc][D]);
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) {
                 const float wgt = exp2_fast(sMerge[w][cc][D] - m);
-                o0 = fmaf(sMerge[w][cc][e], wgt, o0);
-                o1 = fmaf(sMerge[w][cc][e + 1], wgt, o1);
+                o += *reinterpret_cast<const f32x4_t*>(&sMerge[w][cc][e]) * wgt;
                 zz = fmaf(sMerge[w][cc][D + 1], wgt, zz);
             }
             const int c = 16 * nt + cc;
-            if (!PageRow<FMT>::kQuantised && (sNotFinite[0] | sNotFinite[1] | sNotFinite[2] | sNotFinite[3])) add_not_finite(first_new + c / g, e, o0, o1);
+            if (!PageRow<FMT>::kQuantised && any_not_finite()) add_not_finite(first_new + c / g, e, o);
             if (nu == 1) {
-                T* out = (T*)a.out.at(l, b, h * g + c % g, c / g) + e;
-                store_pair(out, zz == 0.f ? 0.f : o0 / zz, zz == 0.f ? 0.f : o1 / zz);
-                if (e == 0 && a.stats.row_max) store_stats(a, l, b, h * g + c % g, c / g, m, zz);
-            } else {
-                store_agent2(part + c * D + e, o0, o1);
+                store_out(c, e, o, m, zz);
+            } else if constexpr (ONE_LAUNCH) {                      // device-scope stores
+                store_agent2(part + c * D + e, o[0], o[1]);
+                store_agent2(part + c * D + e + 2, o[2], o[3]);
                 if (e == 0) store_agent2(part + cols * D + 2 * c, m, zz);
+            } else {
+                *reinterpret_cast<f32x4_t*>(part + c * D + e) = o;
+                if (e == 0) *reinterpret_cast<float2*>(part + cols * D + 2 * c) = make_float2(m, zz);
             }
         }
     }
+    if constexpr (!ONE_LAUNCH) return;
     if (nu == 1) return;
     // ---- the unit counts itself once its stores are acknowledged; the last one of the row merges
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -475,58 +563,113 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void pages_few_kernel(Pa
     __syncthreads();
     if (!sLast) return;
     if (tid == 0) __hip_atomic_store(a.counters + row, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    // Two neighbouring outputs per thread; if the block has threads for several times all outputs, the units are dealt to
-    // them, and the groups of threads merge through LDS.
-    const float* parts = a.partials + (int64_t)row * a.n_units * a.part_floats;
-    const int pairs = cols * (D / 2);
-    const int groups = pairs >= kThreads ? 1 : kThreads / pairs;
-    constexpr int NB = 8;                                       // partial results whose loads are in flight together
-    float* sPart = &sMerge[0][0][0];                            // [kThreads][4]
-    for (int x0 = 0; x0 < pairs; x0 += kThreads) {              // one round unless groups == 1
-        const int x = groups == 1 ? x0 + tid : tid % pairs, grp = groups == 1 ? 0 : tid / pairs;
-        float m = kNoMax, o0 = 0.f, o1 = 0.f, z = 0.f;
-        const int c = x / (D / 2), e = x % (D / 2) * 2;
-        if (x < pairs && grp < groups)
+    // Four neighbouring outputs per thread and round, the loads of all rounds and of NB units in flight together; if the block
+    // has threads for several times all outputs, the units are dealt to them, and the groups of threads merge through LDS.
+    constexpr int ROUNDS = (16 * (D / 4) + kThreads - 1) / kThreads, NB = 8;
+    const auto parts = partials_buffer(a.partials + (int64_t)row * a.n_units * a.part_floats, nu * a.part_floats * 4);
+    const int quads = cols * (D / 4);
+    const int groups = quads >= kThreads ? 1 : kThreads / quads;
+    const int x0 = groups == 1 ? tid : tid % quads, grp = groups == 1 ? 0 : tid / quads;
+    float m[ROUNDS], z[ROUNDS];
+    f32x4_t o[ROUNDS];
+#pragma unroll
+    for (int k = 0; k < ROUNDS; ++k) { m[k] = kNoMax; z[k] = 0.f; o[k] = f32x4_t{0.f, 0.f, 0.f, 0.f}; }
 #pragma unroll 1
-            for (int u0 = grp; u0 < nu; u0 += NB * groups) {
-                float2 ml[NB], ov[NB];
+    for (int u0 = grp; u0 < nu; u0 += NB * groups) {
+        float2 ml[ROUNDS][NB];
+        f32x4_t ov[ROUNDS][NB];
+#pragma unroll
+        for (int k = 0; k < ROUNDS; ++k)
+            if (k == 0 || k * kThreads < quads) {               // block-uniform
+                const int x = min(x0 + k * kThreads, quads - 1), c = x / (D / 4), e = x % (D / 4) * 4;
 #pragma unroll
                 for (int j = 0; j < NB; ++j) {
-                    const int u = min(u0 + j * groups, nu - 1);
-                    ml[j] = load_agent2(parts + (int64_t)u * a.part_floats + cols * D + 2 * c);
-                    ov[j] = load_agent2(parts + (int64_t)u * a.part_floats + c * D + e);
-                    if (u0 + j * groups >= nu) { ml[j] = make_float2(kNoMax, 0.f); ov[j] = make_float2(0.f, 0.f); }
+                    const int at = min(u0 + j * groups, nu - 1) * a.part_floats * 4;
+                    ml[k][j] = buffer_load8_agent(parts, at + (cols * D + 2 * c) * 4);
+                    ov[k][j] = buffer_load16_agent(parts, at + (c * D + e) * 4);
                 }
-                float mn = m;
-#pragma unroll
-                for (int j = 0; j < NB; ++j) mn = fmaxf(mn, ml[j].x);
-                const float w0 = exp2_fast(m - mn);
-                o0 *= w0; o1 *= w0; z *= w0;
-#pragma unroll
-                for (int j = 0; j < NB; ++j) {
-                    const float wgt = exp2_fast(ml[j].x - mn);
-                    o0 = fmaf(ov[j].x, wgt, o0); o1 = fmaf(ov[j].y, wgt, o1); z = fmaf(ml[j].y, wgt, z);
-                }
-                m = mn;
             }
-        if (groups > 1) {
-            __syncthreads();
-            *reinterpret_cast<float4*>(sPart + 4 * tid) = make_float4(m, z, o0, o1);
-            __syncthreads();
-            if (tid < pairs)
-                for (int k = 1; k < groups; ++k) {
-                    const float4 f = *reinterpret_cast<const float4*>(sPart + 4 * (tid + k * pairs));
-                    const float mn = fmaxf(m, f.x), w0 = exp2_fast(m - mn), w1 = exp2_fast(f.x - mn);
-                    o0 = o0 * w0 + f.z * w1; o1 = o1 * w0 + f.w * w1; z = z * w0 + f.y * w1;
-                    m = mn;
+#pragma unroll
+        for (int k = 0; k < ROUNDS; ++k)
+            if (k == 0 || k * kThreads < quads) {
+                float mn = m[k];
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    if (u0 + j * groups >= nu) { ml[k][j] = make_float2(kNoMax, 0.f); ov[k][j] = f32x4_t{0.f, 0.f, 0.f, 0.f}; }
+                    mn = fmaxf(mn, ml[k][j].x);
                 }
-        }
-        if (x < pairs && grp == 0) {
-            T* out = (T*)a.out.at(l, b, h * g + c % g, c / g) + e;
-            store_pair(out, z == 0.f ? 0.f : o0 / z, z == 0.f ? 0.f : o1 / z);
-            if (e == 0 && a.stats.row_max) store_stats(a, l, b, h * g + c % g, c / g, m, z);
-        }
+                const float w0 = exp2_fast(m[k] - mn);
+                o[k] *= w0; z[k] *= w0;
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    const float wgt = exp2_fast(ml[k][j].x - mn);
+                    o[k] += ov[k][j] * wgt;
+                    z[k] = fmaf(ml[k][j].y, wgt, z[k]);
+                }
+                m[k] = mn;
+            }
     }
+    if (groups > 1) {
+        float* sPart = &sMerge[0][0][0];                        // [kThreads][6]
+        float* mine = sPart + 6 * tid;
+        mine[0] = m[0]; mine[1] = z[0]; mine[2] = o[0][0]; mine[3] = o[0][1]; mine[4] = o[0][2]; mine[5] = o[0][3];
+        __syncthreads();
+        if (tid < quads)
+            for (int k = 1; k < groups; ++k) {
+                const float* f = sPart + 6 * (tid + k * quads);
+                const float mn = fmaxf(m[0], f[0]), w0 = exp2_fast(m[0] - mn), w1 = exp2_fast(f[0] - mn);
+                o[0] = o[0] * w0 + f32x4_t{f[2], f[3], f[4], f[5]} * w1;
+                z[0] = z[0] * w0 + f[1] * w1;
+                m[0] = mn;
+            }
+    }
+#pragma unroll
+    for (int k = 0; k < ROUNDS; ++k) {
+        const int x = x0 + k * kThreads, c = x / (D / 4), e = x % (D / 4) * 4;
+        if (grp != 0 || x >= quads) break;
+        store_out(c, e, o[k], m[k], z[k]);
+    }
+}
+
+// Merge of the units of a row, four neighbouring outputs per thread.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void pages_few_merge_kernel(PagesAttnParams a) {
+    const int row = blockIdx.y, h = row % a.p.Hkv, lb = row / a.p.Hkv, b = lb % a.p.B, l = lb / a.p.B;
+    const ChunkLen len = chunk_len(a.p, b);
+    const int nu = (len.n + (1 << a.unit_shift) - 1) >> a.unit_shift, cols = a.p.g * len.c;
+    const int x = blockIdx.x * 256 + threadIdx.x, c = x / (D / 4), e = x % (D / 4) * 4;
+    if (nu < 2 || c >= cols) return;
+    const float* part = a.partials + (int64_t)row * a.n_units * a.part_floats;
+    constexpr int NB = 8;
+    float m = kNoMax, z = 0.f;
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int u0 = 0; u0 < nu; u0 += NB) {
+        float2 ml[NB];
+        f32x4_t ov[NB];
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const float* p = part + (int64_t)min(u0 + j, nu - 1) * a.part_floats;
+            ml[j] = *reinterpret_cast<const float2*>(p + cols * D + 2 * c);
+            ov[j] = *reinterpret_cast<const f32x4_t*>(p + c * D + e);
+        }
+        float mn = m;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            if (u0 + j >= nu) { ml[j] = make_float2(kNoMax, 0.f); ov[j] = f32x4_t{0.f, 0.f, 0.f, 0.f}; }
+            mn = fmaxf(mn, ml[j].x);
+        }
+        const float w0 = exp2_fast(m - mn);
+        o *= w0; z *= w0;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const float wgt = exp2_fast(ml[j].x - mn);
+            o += ov[j] * wgt;
+            z = fmaf(ml[j].y, wgt, z);
+        }
+        m = mn;
+    }
+    store_column<T>(a, l, b, h, c, e, o, m, z);
 }
 
 struct FewPlan { int unit_shift, n_units, part_floats; size_t bytes; };
@@ -535,8 +678,18 @@ FewPlan plan(const PagesCall& c) {
     FewPlan f;
     const int ps_shift = __builtin_ctz(c.s.page_slots);
     const int64_t rows = (int64_t)c.n_layers * c.chunk.B * c.s.Hkv;
-    f.unit_shift = 7;
-    while (f.unit_shift < 10 && f.unit_shift < ps_shift + 6 && rows * ((c.chunk.max_len >> f.unit_shift) + 1) > 2048) ++f.unit_shift;
+    // Units so long that about 192 blocks cover the call: three quarters of the compute units start at once, and few partial
+    // results wait for each other; a request of up to 512 positions is one unit and has none.  Where even 2048 positions make
+    // more blocks than that, 1024, which balance requests of different lengths better.  us of one layer, eight KV heads of four
+    // query heads, units of 128 / 256 / 512 / 1024 / 2048: one request of 2945 positions 10.1 / 9.1 / 11.0 / 15.4 / 23.3, of 300
+    // 8.7 / 8.8 / 8.2, of 1000 9.3 / 10.1 / 12.3 (so 128 up to 64 positions a block), of 10000 19.7 / 15.4 / 13.7 / 16.2 / 24.7, of 32768 48.4 / 33.4 / 27.9 / 25.6 / 25.5;
+    // four of 10368 48.6 / 35.3 / 31.9 / 32.7 / 29.0; 24 of up to 10369 (FP8) 99.5 / 67.3 / 53.7 / 54.7 / 57.3.
+    const int64_t per_block = rows * c.chunk.max_len / 192;
+    f.unit_shift = per_block > 64 ? 8 : 7;
+    while (f.unit_shift < 11 && per_block * 10 > (int64_t)14 << f.unit_shift) ++f.unit_shift;
+    if (per_block * 10 > (int64_t)14 << 11) f.unit_shift = 10;
+    if (c.chunk.max_len <= 512) f.unit_shift = 9;
+    if (f.unit_shift > ps_shift + 6) f.unit_shift = ps_shift + 6;          // a wave holds the page ids of a unit, a lane each
     f.n_units = (c.chunk.max_len + (1 << f.unit_shift) - 1) >> f.unit_shift;
     const int cols = c.s.Hq / c.s.Hkv * c.chunk.max_new;
     f.part_floats = (cols * (c.s.d + 2) + 3) & ~3;
@@ -546,14 +699,23 @@ FewPlan plan(const PagesCall& c) {
 
 template <int D, int FMT>
 void launch(const PagesAttnParams& a, int cols, hipStream_t st) {
-    const unsigned grid = (unsigned)(a.p.n_layers * a.p.B * a.p.Hkv) * a.n_units;
-    if (cols <= 16) pages_few_kernel<D, FMT, 1><<<grid, kThreads, 0, st>>>(a);
-    else pages_few_kernel<D, FMT, 2><<<grid, kThreads, 0, st>>>(a);
+    const int rows = a.p.n_layers * a.p.B * a.p.Hkv;
+    const dim3 grid(a.p.Hkv, a.p.n_layers * a.p.B, a.n_units);
+    if (cols <= 16) {
+        pages_few_kernel<D, FMT, 1><<<grid, kThreads, 0, st>>>(a);
+        return;
+    }
+    if (cols <= 32) pages_few_kernel<D, FMT, 2><<<grid, kThreads, 0, st>>>(a);
+    else if constexpr (FMT != kPageF32) {
+        if (cols <= 48) pages_few_kernel<D, FMT, 3><<<grid, kThreads, 0, st>>>(a);
+        else pages_few_kernel<D, FMT, 4><<<grid, kThreads, 0, st>>>(a);
+    }
+    if (a.n_units > 1) pages_few_merge_kernel<typename PageRow<FMT>::T, D><<<dim3((cols * (D / 4) + 255) / 256, rows), 256, 0, st>>>(a);
 }
 
 }  // namespace
 
-bool pages_few_supported(const PagesCall& c) { return (int64_t)(c.s.Hq / c.s.Hkv) * c.chunk.max_new <= 32; }
+bool pages_few_supported(const PagesCall& c) { return (int64_t)(c.s.Hq / c.s.Hkv) * c.chunk.max_new <= (c.s.dtype == VLC_F32 ? 32 : 64); }
 size_t pages_few_workspace_bytes(const PagesCall& c) { return plan(c).bytes; }
 
 hipError_t launch_pages_few(const PagesAttn& c) {

@@ -232,7 +232,6 @@ __global__ __launch_bounds__(kThreads, 1) void pages_rows_kernel(RowsArgs ra) {
         v_at[dt] = lds_address(&sV[0][v_place<D>(key, el >> 3)]) + (el & 4) * 2;
     }
     auto step_offset = [&](int j) { return (uint32_t)((j & (2 * kRing - 1)) * kStep); };
-    typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
     typedef const __attribute__((address_space(3))) u32x4_t* LdsPieces;
     bf16x8_t kf[KS];
     auto load_k = [&](int j) {         // fragments of the keys of step j; behind the last one: of whatever the ring holds there
