@@ -17,7 +17,7 @@
 // three stages ahead; codes are fetched into registers, expanded to bf16 (exactly) on their way into LDS, and their scales
 // multiply the logits and the probabilities.  16-byte pieces of a row lie at swizzled places, so that neither the reads of K
 // (16 rows, one piece) nor the transposing reads of V (four rows, 64 bytes) meet on a bank.
-#include "pages_attn.h"
+#include "pages_rows.h"
 #include "score_tiles.h"
 
 namespace vlc {
@@ -29,14 +29,6 @@ constexpr int kWaves = 4, kThreads = kWaves * 64;
 constexpr int kStage = 64;             // keys per stage
 constexpr int kRing = 4;
 constexpr float kSlack = 10.f;
-
-struct RowsArgs {
-    PagesAttnParams a;
-    int row_blocks, groups;            // of a KV head's rows; layers * requests * KV heads
-    int stages_per_split;
-    float* part_o;                     // [group][split][rows][D] unnormalised
-    float2* part_mz;                   // [group][split][rows]
-};
 
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
@@ -62,7 +54,7 @@ __device__ __forceinline__ float max_across_halves(float x) {
 }
 
 template <int D, int FMT, int RB>
-__global__ __launch_bounds__(kThreads, 1) void pages_rows_kernel(RowsArgs ra) {
+__global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void pages_rows_kernel(PagesRowsParams ra) {
     constexpr bool Q8 = PageRow<FMT>::kQuantised;
     constexpr int KS = D / 16, DT = D / 32, PPR = D / 8;       // k-steps of K Q^T, 32-wide tiles of d, pieces per row
     constexpr int ROWB = D * PageRow<FMT>::kElemBytes;         // bytes of a row in a page
@@ -92,7 +84,7 @@ __global__ __launch_bounds__(kThreads, 1) void pages_rows_kernel(RowsArgs ra) {
     if (r0 >= rows) return;
     const int first_last = first_new + r0 / g;                 // last key of the block's first row, and of its last row
     const int last_last = first_new + (min(r0 + 128 * RB, rows) - 1) / g;
-    const int st0 = split * ra.stages_per_split, st1 = min(last_last / kStage + 1, st0 + ra.stages_per_split);
+    const int st0 = split * ra.steps_per_split, st1 = min(last_last / kStage + 1, st0 + ra.steps_per_split);
     const int st_masked = (first_last + 1) / kStage;           // first stage that some row does not see to its end
 
     const float scale = attn_scale(a, l, D), c = tiles::exp_scale(scale);
@@ -165,38 +157,40 @@ __global__ __launch_bounds__(kThreads, 1) void pages_rows_kernel(RowsArgs ra) {
     };
     // codes: a thread fetches 16 at a time
     constexpr int CPR = D / 16, CODE_LOADS = kStage * CPR / kThreads > 0 ? kStage * CPR / kThreads : 1;
-    uint4 kc[Q8 ? CODE_LOADS : 1], vc[Q8 ? CODE_LOADS : 1];
-    float sc = 0.f;
+    struct Codes {
+        uint4 k[Q8 ? CODE_LOADS : 1], v[Q8 ? CODE_LOADS : 1];
+        float scale;
+    } codes;
     auto row_of_lane = [&](int key) {
         const int v = __shfl(ids, (key >> a.p.ps_shift) - id_base, kWave);
         return ((head0 + (int64_t)v * a.p.Hkv) << a.p.ps_shift) + (key & ((1 << a.p.ps_shift) - 1));
     };
-    auto request_codes = [&](int st) {
+    auto request_codes = [&](int st, Codes& c8) {
         const int key0 = st * kStage;
         need_ids(key0);
 #pragma unroll
         for (int u = 0; u < CODE_LOADS; ++u) {
             const int x = tid + kThreads * u, r = x / CPR, piece = x % CPR;
             const int64_t row = row_of_lane(key0 + r);
-            kc[u] = *reinterpret_cast<const uint4*>(a.p.k + row * ROWB + piece * 16);
-            vc[u] = *reinterpret_cast<const uint4*>(a.p.v + row * ROWB + piece * 16);
+            c8.k[u] = *reinterpret_cast<const uint4*>(a.p.k + row * ROWB + piece * 16);
+            c8.v[u] = *reinterpret_cast<const uint4*>(a.p.v + row * ROWB + piece * 16);
         }
         const int64_t row = row_of_lane(key0 + lane);          // waves 0 and 1: the scales
-        if (wave < 2) sc = (wave ? a.p.v_scale : a.p.k_scale)[row];
+        if (wave < 2) c8.scale = (wave ? a.p.v_scale : a.p.k_scale)[row];
     };
-    auto store_codes = [&](int st) {
+    auto store_codes = [&](int st, const Codes& c8) {
         const int key0 = st * kStage, buf = st & (kRing - 1);
 #pragma unroll
         for (int u = 0; u < CODE_LOADS; ++u) {
             const int x = tid + kThreads * u, r = x / CPR, piece = x % CPR;
             const bool there = key0 + r < len.n;               // stale codes may stand for NaN
-            const uint4 v = there ? vc[u] : make_uint4(0, 0, 0, 0);
-            sK[buf][k_place<D>(r, 2 * piece)] = codes_to_bf16<FMT>(make_uint2(kc[u].x, kc[u].y));
-            sK[buf][k_place<D>(r, 2 * piece + 1)] = codes_to_bf16<FMT>(make_uint2(kc[u].z, kc[u].w));
+            const uint4 v = there ? c8.v[u] : make_uint4(0, 0, 0, 0);
+            sK[buf][k_place<D>(r, 2 * piece)] = codes_to_bf16<FMT>(make_uint2(c8.k[u].x, c8.k[u].y));
+            sK[buf][k_place<D>(r, 2 * piece + 1)] = codes_to_bf16<FMT>(make_uint2(c8.k[u].z, c8.k[u].w));
             sV[buf][v_place<D>(r, 2 * piece)] = codes_to_bf16<FMT>(make_uint2(v.x, v.y));
             sV[buf][v_place<D>(r, 2 * piece + 1)] = codes_to_bf16<FMT>(make_uint2(v.z, v.w));
         }
-        if (wave < 2) (wave ? sVs : sKs)[buf][lane] = wave ? sc : sc * c;
+        if (wave < 2) (wave ? sVs : sKs)[buf][lane] = wave ? c8.scale : c8.scale * c;
     };
 
     auto barrier = [&]() {
@@ -343,9 +337,9 @@ __global__ __launch_bounds__(kThreads, 1) void pages_rows_kernel(RowsArgs ra) {
             barrier();
             if (st + 3 < st1) request_plain(st + 3);
         } else {
-            if (st + 2 < st1) store_codes(st + 2);
+            if (st + 2 < st1) store_codes(st + 2, codes);
             barrier();
-            if (st + 3 < st1) request_codes(st + 3);
+            if (st + 3 < st1) request_codes(st + 3, codes);
         }
     };
 
@@ -359,10 +353,12 @@ __global__ __launch_bounds__(kThreads, 1) void pages_rows_kernel(RowsArgs ra) {
             else if (st0 + 1 < st1) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(LOADS) : "memory");
             else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         } else {
-            request_codes(st0);
-            store_codes(st0);
-            if (st0 + 1 < st1) { request_codes(st0 + 1); store_codes(st0 + 1); }
-            if (st0 + 2 < st1) request_codes(st0 + 2);
+            Codes first, second;
+            request_codes(st0, first);
+            if (st0 + 1 < st1) request_codes(st0 + 1, second);
+            if (st0 + 2 < st1) request_codes(st0 + 2, codes);
+            store_codes(st0, first);
+            if (st0 + 1 < st1) store_codes(st0 + 1, second);
         }
         barrier();
         if (st0 >= st_masked) clean_v(st0);
@@ -454,47 +450,7 @@ __global__ __launch_bounds__(kThreads, 1) void pages_rows_kernel(RowsArgs ra) {
     }
 }
 
-// Merge of the key splits: D / 4 lanes per row.  A split beyond what the row's block saw has left nothing: kNoMax and 0 are
-// written by its block all the same.
-template <int D>
-__global__ __launch_bounds__(256) void pages_rows_merge_kernel(RowsArgs ra) {
-    const PagesAttnParams& a = ra.a;
-    constexpr int LPR = D / 4;
-    const int sub = threadIdx.x % LPR;
-    const int group = blockIdx.y, h = group % a.p.Hkv, lb = group / a.p.Hkv, b = lb % a.p.B, l = lb / a.p.B;
-    const int r = blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
-    const int g = a.p.g;
-    if (r >= g * chunk_len(a.p, b).c) return;
-    const int64_t stride = (int64_t)g * a.p.max_new, p0 = (int64_t)group * a.n_units * stride + r;
-    float m = kNoMax, z = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    constexpr int NB = 4;
-    for (int s0 = 0; s0 < a.n_units; s0 += NB) {
-        float2 mz[NB];
-        float4 f[NB];
-#pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            const int64_t at = p0 + min(s0 + j, a.n_units - 1) * stride;
-            mz[j] = ra.part_mz[at];
-            f[j] = *reinterpret_cast<const float4*>(ra.part_o + at * D + sub * 4);
-        }
-#pragma unroll
-        for (int j = 0; j < NB; ++j)
-            if (s0 + j < a.n_units) {
-                const float mn = fmaxf(m, mz[j].x), w0 = exp2_fast(m - mn), w1 = exp2_fast(mz[j].x - mn);
-                z = z * w0 + mz[j].y * w1;
-                o.x = o.x * w0 + f[j].x * w1; o.y = o.y * w0 + f[j].y * w1; o.z = o.z * w0 + f[j].z * w1; o.w = o.w * w0 + f[j].w * w1;
-                m = mn;
-            }
-    }
-    const float inv = z == 0.f ? 0.f : 1.f / z;
-    bf16_t* out = (bf16_t*)a.out.at(l, b, h * g + r % g, r / g) + sub * 4;
-    store_pair(out, o.x * inv, o.y * inv);
-    store_pair(out + 2, o.z * inv, o.w * inv);
-    if (sub == 0 && a.stats.row_max) store_stats(a, l, b, h * g + r % g, r / g, m, z);
-}
-
-struct RowsPlan { int rb, row_blocks, splits, stages_per_split; int64_t groups, rows; size_t o_bytes, bytes; };
+struct RowsPlan { int rb, row_blocks, splits, steps_per_split; int64_t groups, rows; size_t o_bytes, bytes; };
 
 RowsPlan plan(const PagesCall& c) {
     RowsPlan p;
@@ -505,33 +461,31 @@ RowsPlan plan(const PagesCall& c) {
     p.row_blocks = (int)((p.rows + 128 * p.rb - 1) / (128 * p.rb));
     const int stages = (c.chunk.max_len + kStage - 1) / kStage;
     const int64_t blocks = p.groups * p.row_blocks;
-    // A block fills a compute unit; a launch takes as many rounds as it has blocks per 256.  Splitting the keys fills the last
+    // A block fills a compute unit (d = 64: half of one); a launch takes as many rounds as it has blocks per 256.  Splitting the keys fills the last
     // round, for a start and an end of about four stages per block and the way of the partial results through memory.
+    const int resident = c.s.d == 64 ? 512 : 256;
     int best = 1;
     double least = 1e300;
     for (int ns = 1; ns <= 64 && ns * 4 <= stages + 3 && (ns == 1 || blocks * ns <= 8192); ++ns) {
         const int per = (stages + ns - 1) / ns;
-        double cost = (double)((blocks * ns + 255) / 256) * (per + 4);
+        double cost = (double)((blocks * ns + resident - 1) / resident) * (per + 4);
         if (ns > 1) cost += 4 + (double)p.groups * p.rows * ns * c.s.d * 8 / 4.0e6;
         if (cost < least) { least = cost; best = ns; }
     }
-    p.stages_per_split = (stages + best - 1) / best;
-    p.splits = (stages + p.stages_per_split - 1) / p.stages_per_split;
+    p.steps_per_split = (stages + best - 1) / best;
+    p.splits = (stages + p.steps_per_split - 1) / p.steps_per_split;
     const size_t n = (size_t)p.groups * p.splits * p.rows;
-    p.o_bytes = (n * c.s.d * sizeof(float) + 255) / 256 * 256;
+    p.o_bytes = pages_partials_o_bytes(n, c.s.d);
     p.bytes = p.splits > 1 ? p.o_bytes + n * sizeof(float2) : 0;
     return p;
 }
 
 template <int D, int FMT>
-void launch(const RowsArgs& ra, int rb, hipStream_t st) {
+void launch(const PagesRowsParams& ra, int rb, hipStream_t st) {
     const unsigned grid = (unsigned)ra.groups * ra.row_blocks * ra.a.n_units;
     if (rb == 1) pages_rows_kernel<D, FMT, 1><<<grid, kThreads, 0, st>>>(ra);
     else pages_rows_kernel<D, FMT, 2><<<grid, kThreads, 0, st>>>(ra);
-    if (ra.a.n_units > 1) {
-        constexpr int per = 256 / (D / 4);
-        pages_rows_merge_kernel<D><<<dim3((ra.a.p.g * ra.a.p.max_new + per - 1) / per, ra.groups), 256, 0, st>>>(ra);
-    }
+    if (ra.a.n_units > 1) launch_pages_rows_merge<bf16_t, D>(ra, st);
 }
 
 }  // namespace
@@ -540,10 +494,10 @@ size_t pages_rows_workspace_bytes(const PagesCall& c) { return plan(c).bytes; }
 
 hipError_t launch_pages_rows(const PagesAttn& c) {
     const RowsPlan p = plan(c.c);
-    RowsArgs ra;
+    PagesRowsParams ra;
     ra.a = pages_attn_params(c);
     ra.a.n_units = p.splits;
-    ra.row_blocks = p.row_blocks; ra.groups = (int)p.groups; ra.stages_per_split = p.stages_per_split;
+    ra.row_blocks = p.row_blocks; ra.groups = (int)p.groups; ra.steps_per_split = p.steps_per_split;
     ra.part_o = (float*)c.workspace;
     ra.part_mz = (float2*)((char*)c.workspace + p.o_bytes);
     const bool wide = c.c.s.d == 128;

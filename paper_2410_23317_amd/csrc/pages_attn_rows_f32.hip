@@ -7,7 +7,7 @@
 // O^T += V^T P^T as they are: instruction i of a tile multiplies keys 8 (i / 4) + 4 half + i % 4, which is the order the
 // accumulators have.  K goes through LDS with rows of D + 4 floats, so that the 32 rows of a 16-byte read of a lane half meet
 // each bank equally often; V with rows of D floats, read a number per lane, 32 neighbours.
-#include "pages_attn.h"
+#include "pages_rows.h"
 #include "score_tiles.h"
 
 namespace vlc {
@@ -17,15 +17,8 @@ using tiles::acc_row;
 
 constexpr int kWaves = 4, kThreads = kWaves * 64, kRows = 32 * kWaves, kKeys = 32;
 
-struct RowsF32Args {
-    PagesAttnParams a;
-    int row_blocks, groups, tiles_per_split;
-    float* part_o;                     // [group][split][rows][D] unnormalised
-    float2* part_mz;                   // [group][split][rows]
-};
-
 template <int D>
-__global__ __launch_bounds__(kThreads, 2) void pages_rows_f32_kernel(RowsF32Args ra) {
+__global__ __launch_bounds__(kThreads, 2) void pages_rows_f32_kernel(PagesRowsParams ra) {
     constexpr int KP = D / 8, DT = D / 32, PPR = D / 4, LOADS = kKeys * PPR / kThreads, PITCH = D + 4;
     __shared__ __align__(16) float sK[kKeys * PITCH], sV[kKeys * D];
     __shared__ int sBad[2];            // first and last tile in which numbers of V were replaced by 0
@@ -39,7 +32,7 @@ __global__ __launch_bounds__(kThreads, 2) void pages_rows_f32_kernel(RowsF32Args
     const int g = a.p.g, rows = g * len.c, first_new = len.n - len.c, r0 = rblk * kRows;
     if (r0 >= rows) return;
     const int first_last = first_new + r0 / g, last_last = first_new + (min(r0 + kRows, rows) - 1) / g;
-    const int t0 = split * ra.tiles_per_split, t1 = min(last_last / kKeys + 1, t0 + ra.tiles_per_split);
+    const int t0 = split * ra.steps_per_split, t1 = min(last_last / kKeys + 1, t0 + ra.steps_per_split);
     const int t_masked = (first_last + 1) / kKeys;             // first tile that some row does not see to its end
 
     const int r = min(r0 + 32 * wave + (lane & 31), rows - 1), last = first_new + r / g;
@@ -55,7 +48,7 @@ __global__ __launch_bounds__(kThreads, 2) void pages_rows_f32_kernel(RowsF32Args
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) o[dt] = f32x16_t{0};
 
-    uint4 kr[LOADS], vr[LOADS];
+    f32x4_t kr[LOADS], vr[LOADS];
     auto request = [&](int t) {
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) {
@@ -66,8 +59,8 @@ __global__ __launch_bounds__(kThreads, 2) void pages_rows_f32_kernel(RowsF32Args
                 page = 0;
             }
             const int64_t at = (page_row0(a.p, a.p.layer_begin + l, page, h) + (key & ((1 << a.p.ps_shift) - 1))) * PPR + x % PPR;
-            kr[u] = reinterpret_cast<const uint4*>(a.p.k)[at];
-            vr[u] = reinterpret_cast<const uint4*>(a.p.v)[at];
+            kr[u] = reinterpret_cast<const f32x4_t*>(a.p.k)[at];
+            vr[u] = reinterpret_cast<const f32x4_t*>(a.p.v)[at];
         }
     };
     if (tid < 2) sBad[tid] = tid ? -1 : INT32_MAX;
@@ -79,15 +72,16 @@ __global__ __launch_bounds__(kThreads, 2) void pages_rows_f32_kernel(RowsF32Args
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) {
             const int x = tid + kThreads * u;
-            *reinterpret_cast<uint4*>(&sK[x / PPR * PITCH + x % PPR * 4]) = kr[u];
+            *reinterpret_cast<f32x4_t*>(&sK[x / PPR * PITCH + x % PPR * 4]) = kr[u];
+            f32x4_t f = vr[u];
             if (t >= t_masked) {       // numbers of V that are not finite become 0 where a row does not see them (0 times them is no 0)
-                uint4& w = vr[u];
-                const uint4 f = make_uint4(is_finite(__uint_as_float(w.x)) ? w.x : 0, is_finite(__uint_as_float(w.y)) ? w.y : 0,
-                                           is_finite(__uint_as_float(w.z)) ? w.z : 0, is_finite(__uint_as_float(w.w)) ? w.w : 0);
-                bad |= f.x != w.x || f.y != w.y || f.z != w.z || f.w != w.w;
-                w = f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    bad |= !is_finite(f[e]);
+                    f[e] = is_finite(f[e]) ? f[e] : 0.f;
+                }
             }
-            *reinterpret_cast<uint4*>(&sV[x * 4]) = vr[u];
+            *reinterpret_cast<f32x4_t*>(&sV[x * 4]) = f;
         }
         if (bad) { atomicMin(&sBad[0], t); atomicMax(&sBad[1], t); }
         __syncthreads();
@@ -158,32 +152,7 @@ __global__ __launch_bounds__(kThreads, 2) void pages_rows_f32_kernel(RowsF32Args
     }
 }
 
-// Merge of the key splits: D / 4 lanes per row.
-template <int D>
-__global__ __launch_bounds__(256) void pages_rows_f32_merge_kernel(RowsF32Args ra) {
-    const PagesAttnParams& a = ra.a;
-    constexpr int LPR = D / 4;
-    const int sub = threadIdx.x % LPR;
-    const int group = blockIdx.y, h = group % a.p.Hkv, lb = group / a.p.Hkv, b = lb % a.p.B, l = lb / a.p.B;
-    const int r = blockIdx.x * (256 / LPR) + threadIdx.x / LPR, g = a.p.g;
-    if (r >= g * chunk_len(a.p, b).c) return;
-    const int64_t stride = (int64_t)g * a.p.max_new, p0 = (int64_t)group * a.n_units * stride + r;
-    float m = kNoMax, z = 0.f;
-    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < a.n_units; ++s) {
-        const float2 mz = ra.part_mz[p0 + s * stride];
-        const f32x4_t f = *reinterpret_cast<const f32x4_t*>(ra.part_o + (p0 + s * stride) * D + sub * 4);
-        const float mn = fmaxf(m, mz.x), w0 = exp2_fast(m - mn), w1 = exp2_fast(mz.x - mn);
-        z = z * w0 + mz.y * w1;
-        o = o * w0 + f * w1;
-        m = mn;
-    }
-    float* out = (float*)a.out.at(l, b, h * g + r % g, r / g) + sub * 4;
-    *reinterpret_cast<float4*>(out) = z == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o[0] / z, o[1] / z, o[2] / z, o[3] / z);
-    if (sub == 0 && a.stats.row_max) store_stats(a, l, b, h * g + r % g, r / g, m, z);
-}
-
-struct Plan { int row_blocks, splits, tiles_per_split; int64_t groups, rows; size_t o_bytes, bytes; };
+struct Plan { int row_blocks, splits, steps_per_split; int64_t groups, rows; size_t o_bytes, bytes; };
 
 Plan plan(const PagesCall& c) {
     Plan p;
@@ -192,21 +161,21 @@ Plan plan(const PagesCall& c) {
     p.row_blocks = (int)((p.rows + kRows - 1) / kRows);
     const int tiles = (c.chunk.max_len + kKeys - 1) / kKeys;
     const int64_t blocks = p.groups * p.row_blocks;
-    int ns = blocks >= 512 ? 1 : (int)((512 + blocks - 1) / blocks);        // two blocks a compute unit
-    if (ns > (tiles + 3) / 4) ns = (tiles + 3) / 4;
-    p.tiles_per_split = (tiles + ns - 1) / ns;
-    p.splits = (tiles + p.tiles_per_split - 1) / p.tiles_per_split;
+    // two blocks a compute unit, two tiles at least for each
+    int ns = blocks >= 512 ? 1 : (int)((512 + blocks - 1) / blocks);
+    if (ns > (tiles + 1) / 2) ns = (tiles + 1) / 2;
+    p.steps_per_split = (tiles + ns - 1) / ns;
+    p.splits = (tiles + p.steps_per_split - 1) / p.steps_per_split;
     const size_t n = (size_t)p.groups * p.splits * p.rows;
-    p.o_bytes = (n * c.s.d * sizeof(float) + 255) / 256 * 256;
+    p.o_bytes = pages_partials_o_bytes(n, c.s.d);
     p.bytes = p.splits > 1 ? p.o_bytes + n * sizeof(float2) : 0;
     return p;
 }
 
 template <int D>
-void launch(const RowsF32Args& ra, hipStream_t st) {
+void launch(const PagesRowsParams& ra, hipStream_t st) {
     pages_rows_f32_kernel<D><<<(unsigned)ra.groups * ra.row_blocks * ra.a.n_units, kThreads, 0, st>>>(ra);
-    constexpr int per = 256 / (D / 4);
-    if (ra.a.n_units > 1) pages_rows_f32_merge_kernel<D><<<dim3((ra.a.p.g * ra.a.p.max_new + per - 1) / per, ra.groups), 256, 0, st>>>(ra);
+    if (ra.a.n_units > 1) launch_pages_rows_merge<float, D>(ra, st);
 }
 
 }  // namespace
@@ -215,10 +184,10 @@ size_t pages_rows_f32_workspace_bytes(const PagesCall& c) { return plan(c).bytes
 
 hipError_t launch_pages_rows_f32(const PagesAttn& c) {
     const Plan p = plan(c.c);
-    RowsF32Args ra;
+    PagesRowsParams ra;
     ra.a = pages_attn_params(c);
     ra.a.n_units = p.splits;
-    ra.row_blocks = p.row_blocks; ra.groups = (int)p.groups; ra.tiles_per_split = p.tiles_per_split;
+    ra.row_blocks = p.row_blocks; ra.groups = (int)p.groups; ra.steps_per_split = p.steps_per_split;
     ra.part_o = (float*)c.workspace;
     ra.part_mz = (float2*)((char*)c.workspace + p.o_bytes);
     if (c.c.s.d == 128) launch<128>(ra, c.c.stream);
