@@ -87,6 +87,23 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void pages_rows_kernel(P
     const int st0 = split * ra.steps_per_split, st1 = min(last_last / kStage + 1, st0 + ra.steps_per_split);
     const int st_masked = (first_last + 1) / kStage;           // first stage that some row does not see to its end
 
+    // ---- stages: page ids of 64 pages in a register, a lane each
+    const int64_t head0 = (int64_t)(a.p.layer_begin + l) * a.p.n_pages * a.p.Hkv + h;
+    const int last_page = (len.n - 1) >> a.p.ps_shift;
+    int id_base = INT32_MIN, ids = 0;
+    auto need_ids = [&](int key0) {
+        const int p0 = key0 >> a.p.ps_shift;
+        if (p0 + ((kStage - 1) >> a.p.ps_shift) < id_base + 64 && id_base >= 0) return;
+        id_base = p0;
+        const int page = p0 + lane;
+        int v = page <= last_page ? a.p.table[(int64_t)b * a.p.max_pages + page] : 0;
+        if ((uint32_t)v >= (uint32_t)a.p.n_pages) {
+            set_sticky(a.p.status, VLC_ERR_INVALID_ARG, b, kStickyPage, v);
+            v = 0;
+        }
+        ids = v;
+    };
+    if (st0 < st1) need_ids(st0 * kStage);                     // in front of the requests for Q: what K and V wait for
     const float scale = attn_scale(a, l, D), c = tiles::exp_scale(scale);
     bf16x8_t qf[RB][KS];
     int last[RB];
@@ -119,22 +136,6 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void pages_rows_kernel(P
         for (int dt = 0; dt < DT; ++dt) o[rb][dt] = f32x16_t{0};
     }
 
-    // ---- stages: page ids of 64 pages in a register, a lane each
-    const int64_t head0 = (int64_t)(a.p.layer_begin + l) * a.p.n_pages * a.p.Hkv + h;
-    const int last_page = (len.n - 1) >> a.p.ps_shift;
-    int id_base = INT32_MIN, ids = 0;
-    auto need_ids = [&](int key0) {
-        const int p0 = key0 >> a.p.ps_shift;
-        if (p0 + ((kStage - 1) >> a.p.ps_shift) < id_base + 64 && id_base >= 0) return;
-        id_base = p0;
-        const int page = p0 + lane;
-        int v = page <= last_page ? a.p.table[(int64_t)b * a.p.max_pages + page] : 0;
-        if ((uint32_t)v >= (uint32_t)a.p.n_pages) {
-            set_sticky(a.p.status, VLC_ERR_INVALID_ARG, b, kStickyPage, v);
-            v = 0;
-        }
-        ids = v;
-    };
     // first row (of page_slots) of key's page; keys behind the last one of the request are in its last page, or in page 0
     auto row_of_uniform = [&](int key) {
         const int v = __builtin_amdgcn_readlane(ids, (key >> a.p.ps_shift) - id_base);
@@ -395,34 +396,45 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void pages_rows_kernel(P
     }
     barrier();
     const int64_t prow0 = ((int64_t)group * a.n_units + split) * ((int64_t)g * a.p.max_new);
+    // Through LDS, so that memory sees whole rows: a lane holds 4 neighbouring numbers of d at a time, the wave 32 rows of them.
+    constexpr int PIECES = D / 4;                              // 16-byte pieces of a row of fp32 numbers
+    f32x4_t* sO = reinterpret_cast<f32x4_t*>(wave < 2 ? &sK[0][0] : &sV[0][0]) + (wave & 1) * (32 * PIECES);
+    static_assert(sizeof(sK) >= 2 * 32 * PIECES * 16, "two waves' rows in each half of the ring");
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        const int r = r0 + 32 * (RB * wave + rb) + (lane & 31);
+        const int first = r0 + 32 * (RB * wave + rb), r = first + (lane & 31);
         const float top_m = max_across_halves(peak[rb]), to_top = exp2_fast(m[rb] - top_m);    // relative to the largest logit from here on
         const float zt = (z[rb] + __shfl_xor(z[rb], 32, kWave)) * to_top;
-        if (r >= rows) continue;
-        if (a.n_units == 1) {
-            const float inv = zt == 0.f ? 0.f : to_top / zt;
-            bf16_t* out = (bf16_t*)a.out.at(l, b, h * g + r % g, r / g);
+        const float factor = a.n_units > 1 ? to_top : zt == 0.f ? 0.f : to_top / zt;
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
+        for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                for (int q4 = 0; q4 < 4; ++q4) {
-                    bf16_t* dst = out + dt * 32 + acc_row(4 * q4, lane);
-                    store_pair(dst, o[rb][dt][4 * q4] * inv, o[rb][dt][4 * q4 + 1] * inv);
-                    store_pair(dst + 2, o[rb][dt][4 * q4 + 2] * inv, o[rb][dt][4 * q4 + 3] * inv);
-                }
-            if (half == 0 && a.stats.row_max) store_stats(a, l, b, h * g + r % g, r / g, top_m, zt);
-        } else {
-            float* dst = ra.part_o + (prow0 + r) * D;
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                for (int q4 = 0; q4 < 4; ++q4)
-                    *reinterpret_cast<float4*>(dst + dt * 32 + acc_row(4 * q4, lane)) =
-                        make_float4(o[rb][dt][4 * q4] * to_top, o[rb][dt][4 * q4 + 1] * to_top, o[rb][dt][4 * q4 + 2] * to_top, o[rb][dt][4 * q4 + 3] * to_top);
-            if (half == 0) ra.part_mz[prow0 + r] = make_float2(top_m, zt);
+            for (int q4 = 0; q4 < 4; ++q4) {
+                const f32x4_t x = {o[rb][dt][4 * q4], o[rb][dt][4 * q4 + 1], o[rb][dt][4 * q4 + 2], o[rb][dt][4 * q4 + 3]};
+                sO[(lane & 31) * PIECES + ((dt * 8 + 2 * q4 + half) ^ (lane & (PIECES - 1)))] = x * factor;
+            }
+        if (half == 0 && r < rows) {
+            if (a.n_units > 1) ra.part_mz[prow0 + r] = make_float2(top_m, zt);
+            else if (a.stats.row_max) store_stats(a, l, b, h * g + r % g, r / g, top_m, zt);
         }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the wave's own writes; no other wave touches its rows
+        if (a.n_units > 1) {
+#pragma unroll
+            for (int i = 0; i < 32 * PIECES / 64; ++i) {
+                const int row = (i * 64 + lane) / PIECES, piece = lane % PIECES;
+                if (first + row < rows)
+                    *reinterpret_cast<f32x4_t*>(ra.part_o + (prow0 + first + row) * D + piece * 4) = sO[row * PIECES + (piece ^ (row & (PIECES - 1)))];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16 * PIECES / 64; ++i) {
+                const int row = (i * 64 + lane) / PPR, piece = lane % PPR * 2, rr = first + row;
+                const f32x4_t x = sO[row * PIECES + (piece ^ (row & (PIECES - 1)))], y = sO[row * PIECES + ((piece + 1) ^ (row & (PIECES - 1)))];
+                const bf16x8_t w = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3], (__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
+                if (rr < rows) *reinterpret_cast<bf16x8_t*>(a.out.at(l, b, h * g + rr % g, rr / g) + piece * 8) = w;
+            }
+        }
+        asm volatile("" ::: "memory");
     }
     // What is not finite in V reaches the rows that see it: added to what was just stored, from memory, a number at a time.
     if (!Q8 && sBad[0] < st1) {
@@ -461,16 +473,18 @@ RowsPlan plan(const PagesCall& c) {
     p.row_blocks = (int)((p.rows + 128 * p.rb - 1) / (128 * p.rb));
     const int stages = (c.chunk.max_len + kStage - 1) / kStage;
     const int64_t blocks = p.groups * p.row_blocks;
-    // A block fills a compute unit (d = 64: half of one); a launch takes as many rounds as it has blocks per 256.  Splitting the keys fills the last
-    // round, for a start and an end of about four stages per block and the way of the partial results through memory.
+    // A block fills a compute unit (d = 64: half of one); a launch takes as many rounds as it has blocks per 256 (512).  Splitting
+    // the keys fills the rounds, at the price of a start and an end per block (8 us; a stage takes 2.1 of 256 rows, 1.4 of 128)
+    // and of a second launch through which the partial results go (4 us, and their bytes to memory and back).
     const int resident = c.s.d == 64 ? 512 : 256;
+    const double stage_us = (p.rb == 1 ? 1.4 : 2.1) * (c.s.d == 64 ? 1.1 : 1.0);
     int best = 1;
     double least = 1e300;
-    for (int ns = 1; ns <= 64 && ns * 4 <= stages + 3 && (ns == 1 || blocks * ns <= 8192); ++ns) {
+    for (int ns = 1; ns <= 64 && ns * 2 <= stages + 1 && (ns == 1 || blocks * ns <= 8192); ++ns) {
         const int per = (stages + ns - 1) / ns;
-        double cost = (double)((blocks * ns + resident - 1) / resident) * (per + 4);
-        if (ns > 1) cost += 4 + (double)p.groups * p.rows * ns * c.s.d * 8 / 4.0e6;
-        if (cost < least) { least = cost; best = ns; }
+        double us = (double)((blocks * ns + resident - 1) / resident) * (per * stage_us + 8);
+        if (ns > 1) us += 4 + (double)p.groups * p.rows * ns * c.s.d * 8 / 5.0e6;
+        if (us < least) { least = us; best = ns; }
     }
     p.steps_per_split = (stages + best - 1) / best;
     p.splits = (stages + p.steps_per_split - 1) / p.steps_per_split;
