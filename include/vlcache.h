@@ -423,8 +423,8 @@ typedef struct {
  * + r) * d * elem_size, elem_size being 1 for quantised rows; the V row at v_off plus the same; their scales at
  * k_scale_off / v_scale_off + (((l * n_pages + p) * Hkv + h) * page_slots + r) * 4.  vlc_pages_destroy frees host
  * bookkeeping only.
- * vlc_pages_clear must be enqueued once before any other call on the arena: it resets the sticky status and the counters of
- * the attention, and leaves the pages' rows alone. */
+ * vlc_pages_clear must be enqueued once before any other call that works on the arena (VLC_ERR_INVALID_ARG otherwise): it
+ * resets the sticky status and the counters of the attention, and leaves the pages' rows alone. */
 typedef struct vlc_pages vlc_pages;
 typedef struct {
     size_t status_off;         /* int32[4]: sticky vlc_status, request, kind (-1: page, -2: lengths), detail */

@@ -383,8 +383,10 @@ class Pages:
     def __init__(self, shape: vlc_pages_shape, device="cuda"):
         self.handle = None
         self.shape = shape
+        self.dtype = torch.float32 if shape.dtype == VLC_F32 else torch.bfloat16
         nbytes = vlc_pages_bytes(shape)
         self.arena = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        self.device_index = self.arena.get_device()
         handle = C.c_void_p()
         _check(lib.vlc_pages_create(C.byref(shape), self.arena.data_ptr(), nbytes, C.byref(handle)))
         self.handle = handle
@@ -409,12 +411,12 @@ def vlc_pages_create(shape: vlc_pages_shape, device="cuda") -> Pages:
 
 
 def vlc_pages_clear(pages: Pages) -> None:
-    _check(lib.vlc_pages_clear(pages.handle, _stream()))
+    _check(lib.vlc_pages_clear(pages.handle, _pages_stream(pages)))
 
 
 def vlc_pages_status(pages: Pages) -> None:
     """Synchronises the stream; raises VlcError if the device flagged lengths or a page out of range."""
-    _check(lib.vlc_pages_status(pages.handle, _stream()))
+    _check(lib.vlc_pages_status(pages.handle, _pages_stream(pages)))
 
 
 def make_chunk(table: torch.Tensor, max_new: int, max_len: int, lens: Optional[torch.Tensor] = None) -> vlc_chunk:
@@ -433,18 +435,18 @@ def _rows(t: Optional[torch.Tensor], name: str, pages: Pages, dims) -> Optional[
     """vlc_rows of a tensor [layers, B, heads, rows, d] of any strides, d contiguous."""
     if t is None:
         return None
-    dt = torch.float32 if pages.shape.dtype == VLC_F32 else torch.bfloat16
-    if t.dtype != dt or tuple(t.shape) != tuple(dims):
-        raise ValueError(f"{name} must be {dt} of shape {tuple(dims)}, not {t.dtype} {tuple(t.shape)}")
-    if t.device != pages.arena.device or t.stride(4) != 1:
+    if t.dtype is not pages.dtype or t.shape != dims:
+        raise ValueError(f"{name} must be {pages.dtype} of shape {dims}, not {t.dtype} {tuple(t.shape)}")
+    layer, request, head, row, last = t.stride()
+    if t.get_device() != pages.device_index or last != 1:
         raise ValueError(f"{name} must lie on {pages.arena.device} with its last dimension contiguous")
-    return vlc_rows(t.data_ptr(), *t.stride()[:4])
+    return vlc_rows(t.data_ptr(), layer, request, head, row)
 
 
 def _pages_stream(pages: Pages) -> int:
-    if pages.arena.device.index != torch.cuda.current_device():
+    if pages.device_index != torch.cuda.current_device():
         raise ValueError(f"the pages lie on {pages.arena.device}, which is not the current device")
-    return _stream()
+    return torch._C._cuda_getCurrentRawStream(pages.device_index)
 
 
 def _ref(r):
@@ -455,7 +457,9 @@ def vlc_pages_write(pages: Pages, chunk: vlc_chunk, layer_begin, layer_end, k_ne
     s = pages.shape
     dims = (layer_end - layer_begin, chunk.B, s.Hkv, chunk.max_new, s.d)
     k, v = _rows(k_new, "k_new", pages, dims), _rows(v_new, "v_new", pages, dims)
-    _check(lib.vlc_pages_write(pages.handle, C.byref(chunk), int(layer_begin), int(layer_end), _ref(k), _ref(v), _pages_stream(pages)))
+    st = lib.vlc_pages_write(pages.handle, chunk, layer_begin, layer_end, _ref(k), _ref(v), _pages_stream(pages))
+    if st:
+        _check(st)
 
 
 def vlc_pages_read(pages: Pages, chunk: vlc_chunk, layer_begin, layer_end, first, k_out, v_out) -> None:
@@ -486,13 +490,16 @@ def vlc_pages_attn(pages: Pages, chunk: vlc_chunk, layer_begin, layer_end, q, k_
         raise ValueError("row_max and row_sum come together")
     if row_max is not None:
         for t in (row_max, row_sum):
-            if t.dtype != torch.float32 or tuple(t.shape) != qd[:4] or t.device != pages.arena.device:
+            if t.dtype != torch.float32 or t.shape != qd[:4] or t.get_device() != pages.device_index:
                 raise ValueError(f"row_max and row_sum must be fp32 of shape {qd[:4]} on {pages.arena.device}")
         if row_max.stride() != row_sum.stride() or (chunk.max_new > 1 and row_max.stride(3) != 1):
             raise ValueError("row_max and row_sum must have equal strides and contiguous rows")
         stats = vlc_row_stats(row_max.data_ptr(), row_sum.data_ptr(), *row_max.stride()[:3])
+    if sm_scale is not None and (sm_scale.dtype is not torch.float32 or sm_scale.numel() < s.L or sm_scale.get_device() != pages.device_index):
+        raise ValueError(f"sm_scale must be fp32 of {s.L} numbers on {pages.arena.device}")
     qr, o = _rows(q, "q", pages, qd), _rows(out, "out", pages, qd)
     k, v = _rows(k_new, "k_new", pages, kd), _rows(v_new, "v_new", pages, kd)
-    _check(lib.vlc_pages_attn(pages.handle, C.byref(chunk), int(layer_begin), int(layer_end), _ref(qr), _ref(k), _ref(v), _ptr(sm_scale),
-                              _ref(o), _ref(stats), _ptr(workspace),
-                              0 if workspace is None else workspace.numel() * workspace.element_size(), _pages_stream(pages)))
+    st = lib.vlc_pages_attn(pages.handle, chunk, layer_begin, layer_end, _ref(qr), _ref(k), _ref(v), _ptr(sm_scale), _ref(o), _ref(stats),
+                            _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _pages_stream(pages))
+    if st:
+        _check(st)

@@ -93,6 +93,11 @@ vlc_status check_rows(const char* who, const char* name, const vlc_rows* r, int 
     return VLC_OK;
 }
 
+vlc_status check_cleared(const char* who, const vlc_pages* pages) {
+    if (!pages->cleared) return fail(VLC_ERR_INVALID_ARG, "%s: vlc_pages_clear has not been called on these pages", who);
+    return VLC_OK;
+}
+
 vlc::PagesCall pages_call(const vlc_pages* pages, const vlc_chunk* c, int lb, int le, vlc_stream st) {
     vlc::PagesCall a;
     a.s = pages->shape; a.dev = pages->dev; a.chunk = *c;
@@ -132,12 +137,7 @@ vlc_status vlc_pages_create(const vlc_pages_shape* shape, void* arena, size_t ar
     p->dev.v = base + lay.v_off;
     p->dev.k_scale = (float*)(base + lay.k_scale_off);
     p->dev.v_scale = (float*)(base + lay.v_scale_off);
-    int dev = 0, cus = 0;
-    if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0) {
-        (void)hipGetLastError();
-        cus = 256;
-    }
-    p->num_cus = cus;
+    p->cleared = false;
     *out = p;
     return VLC_OK;
 }
@@ -154,11 +154,13 @@ vlc_status vlc_pages_clear(vlc_pages* pages, vlc_stream stream) {
     if (!pages) return fail(VLC_ERR_INVALID_ARG, "vlc_pages_clear: pages is NULL");
     const hipError_t e = vlc::launch_pages_clear(pages->dev, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(e, "vlc_pages_clear");
+    pages->cleared = true;
     return VLC_OK;
 }
 
 vlc_status vlc_pages_status(vlc_pages* pages, vlc_stream stream) {
     if (!pages) return fail(VLC_ERR_INVALID_ARG, "vlc_pages_status: pages is NULL");
+    if (vlc_status st = check_cleared("vlc_pages_status", pages)) return st;
     int32_t st[4] = {0, 0, 0, 0};
     hipError_t e = hipMemcpyAsync(st, pages->dev.status, sizeof(st), hipMemcpyDeviceToHost, (hipStream_t)stream);
     if (e == hipSuccess) e = hipStreamSynchronize((hipStream_t)stream);
@@ -178,6 +180,7 @@ vlc_status vlc_pages_write(vlc_pages* pages, const vlc_chunk* chunk, int32_t lay
     const vlc_pages_shape& s = pages->shape;
     if (vlc_status st = check_rows(who, "k_new", k_new, s.dtype, false, nl, chunk->B, s.Hkv, chunk->max_new)) return st;
     if (vlc_status st = check_rows(who, "v_new", v_new, s.dtype, false, nl, chunk->B, s.Hkv, chunk->max_new)) return st;
+    if (vlc_status st = check_cleared(who, pages)) return st;
     const hipError_t e = vlc::launch_pages_write(pages_call(pages, chunk, layer_begin, layer_end, stream), *k_new, *v_new);
     if (e != hipSuccess) return hip_fail(e, who);
     return VLC_OK;
@@ -196,6 +199,7 @@ vlc_status vlc_pages_read(vlc_pages* pages, const vlc_chunk* chunk, int32_t laye
     if (first >= chunk->max_len) return VLC_OK;               // no request holds such a position
     if (count > chunk->max_len - first) count = chunk->max_len - first;
     if ((int64_t)count * s.Hkv > 1 << 26) return fail(VLC_ERR_SHAPE, "%s: count * Hkv = %lld exceeds 2^26", who, (long long)count * s.Hkv);
+    if (vlc_status st = check_cleared(who, pages)) return st;
     const hipError_t e = vlc::launch_pages_read(pages_call(pages, chunk, layer_begin, layer_end, stream), first, count, *k_out, *v_out);
     if (e != hipSuccess) return hip_fail(e, who);
     return VLC_OK;
@@ -242,6 +246,7 @@ vlc_status vlc_pages_attn(vlc_pages* pages, const vlc_chunk* chunk, int32_t laye
     if (need && !workspace) return fail(VLC_ERR_INVALID_ARG, "%s: workspace must not be NULL for this call", who);
     if (workspace_bytes < need) return fail(VLC_ERR_CAPACITY, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, need);
     if (need && ((uintptr_t)workspace & 15) != 0) return fail(VLC_ERR_INVALID_ARG, "%s: workspace must be 16-byte aligned", who);
+    if (vlc_status st = check_cleared(who, pages)) return st;
     vlc::PagesAttn a;
     a.c = pages_call(pages, chunk, layer_begin, layer_end, stream);
     a.q = *q; a.out = *out; a.sm_scale = sm_scale; a.workspace = workspace;

@@ -110,7 +110,7 @@ struct vlc_pages {
     vlc_pages_shape shape;
     vlc_pages_layout layout;
     vlc::PagesDev dev;
-    int32_t num_cus;                   // compute units of the device that is current when the handle is created
+    bool cleared;                      // vlc_pages_clear has been enqueued
 };
 
 namespace vlc {

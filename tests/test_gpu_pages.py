@@ -195,6 +195,77 @@ def test_what_a_row_does_not_see_has_no_influence(fmt, dtype, g, cn):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cn", [1, 3, 17, 80, 300])
+def test_numbers_of_v_that_are_not_finite_and_seen(dtype, cn):
+    """A NaN in V anywhere reaches its own column of the rows that see it, and nothing else: in the middle of the keys, in the
+    last keys before the chunk, in the chunk."""
+    n, d = cn + 700, 128
+    spots = [(3, 0), (255, 7), (256, 7), (690, 64), (699, 100), (700, 101), (n - 1, 127)]
+
+    def edit(k, v):
+        for t, e in spots:
+            v[0, 0, 1, t, e] = float("nan")
+    c = U.Case(1, 8, 2, d, [(n, cn)], ps=32, dtype=dtype, k_edit=edit)
+    c.fill()
+    for fresh in (False, True):
+        if fresh:
+            c.pages.arena[c.pages.layout.k_off:] = 255
+            c.fill([n - cn])
+        out, M, Z = c.attn(fresh=fresh)
+        torch.cuda.synchronize()
+        ref = U.attention(c.q[0, 0, :, :cn], U.held(c.k[0, 0], "plain"), U.held(c.v[0, 0], "plain"), c.scale[0].item(), n, cn)
+        U.within(out[0, 0, :, :cn], ref[0], U.bounds(ref, dtype, d, n)[0], f"fresh {fresh}")
+        want = torch.zeros(8, cn, d, dtype=torch.bool)
+        for t, e in spots:
+            want[4:, max(t - 700, 0):, e] = True
+        assert torch.equal(torch.isnan(out[0, 0].cpu()), want)
+
+
+def test_requests_that_share_pages_and_calls_without_lengths():
+    """Two requests continue one prompt: its pages stand in both rows of the table; the lengths are the chunk's bounds."""
+    import paper_2410_23317_amd as V
+    for fmt, cn in (("plain", 1), ("fp8", 4), ("int8", 40)):
+        n, ps = 64 + cn, 32
+        c = U.Case(1, 4, 2, 128, [(n, cn), (n, cn)], ps=ps, fmt=fmt)
+        c.k[0, 1, :, :64], c.v[0, 1, :, :64] = c.k[0, 0, :, :64], c.v[0, 0, :, :64]
+        c.table[1, :2] = c.table[0, :2]
+        one = V.make_chunk(c.table[:1].contiguous(), n, n)               # request 0 writes the shared prompt and its own tokens
+        V.vlc_pages_write(c.pages, one, 0, 1, c.k[:, :1], c.v[:, :1])
+        chunk = V.make_chunk(c.table, cn, n)
+        out, M, Z = c.attn(fresh=True, chunk=chunk)
+        V.vlc_pages_status(c.pages)
+        c.check(out, M, Z, f"{fmt} shared")
+
+
+def test_refusals_of_the_binding():
+    import paper_2410_23317_amd as V
+    c = U.Case(2, 4, 2, 64, [(40, 3)])
+    c.fill()
+    out, ws = torch.empty_like(c.q), torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    k_new, v_new = c.new_rows()
+
+    def attn(q=c.q, k=None, v=None, scale=c.scale, o=out, m=None, z=None, w=ws, lb=0, le=2):
+        V.vlc_pages_attn(c.pages, c.chunk, lb, le, q, k, v, scale, o, m, z, w)
+    attn()
+    stat = torch.empty((2, 1, 4, 3), device="cuda")
+    for kw in (dict(q=c.q.float()), dict(q=c.q[:1]), dict(q=c.q.cpu()), dict(o=out[..., :2, :]), dict(q=c.q.transpose(3, 4).contiguous().transpose(3, 4)),
+               dict(k=k_new.float(), v=v_new), dict(scale=c.scale.double()), dict(scale=c.scale[:1]), dict(m=stat), dict(m=stat, z=stat[:1]),
+               dict(m=stat, z=stat.transpose(2, 3).contiguous().transpose(2, 3)), dict(m=stat.double(), z=stat)):
+        with pytest.raises(ValueError):
+            attn(**kw)
+    for kw in (dict(k=k_new), dict(v=v_new), dict(lb=1, le=1), dict(o=out[:, :, :1].expand(2, 1, 4, 3, 64))):
+        if "lb" in kw:
+            kw.update(q=c.q[:0], o=out[:0])
+        with pytest.raises(V.VlcError):
+            attn(**kw)
+    for bad in (lambda: V.make_chunk(c.table.long(), 3, 40), lambda: V.make_chunk(c.table[0], 3, 40), lambda: V.make_chunk(c.table.cpu(), 3, 40),
+                lambda: V.make_chunk(c.table, 3, 40, c.lens_t[0])):
+        with pytest.raises(ValueError):
+            bad()
+    V.vlc_pages_status(c.pages)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("cn", [1, 5, 20, 90])
 def test_logits_that_are_infinite(dtype, cn):
     """Keys whose logits are all -inf weigh nothing; a row that has no others is 0 with M = -inf and Z = 0."""

@@ -100,7 +100,8 @@ def test_calls_are_refused_before_any_launch(V):
             assert call(lb=lb, le=le) == inv
         for kw in (dict(table=None), dict(table=4098), dict(lens=4097)):
             assert call(chunk=C.byref(chunk_of(V, **kw))) == inv, kw
-        for kw in (dict(B=0), dict(max_pages=0), dict(max_new=0), dict(max_new=301), dict(max_len=321), dict(B=16384, max_new=1)):
+        for kw in (dict(B=0), dict(max_pages=0), dict(max_new=0), dict(max_new=301), dict(max_len=321), dict(B=16384, max_new=1), dict(max_pages=1 << 22, max_len=(1 << 25) + 1),
+                   dict(B=300, max_pages=1 << 21, max_len=1 << 25)):
             assert call(chunk=C.byref(chunk_of(V, **kw))) == shp, kw
         reserved = chunk_of(V)
         reserved.reserved[1] = 1
@@ -129,6 +130,10 @@ def test_calls_are_refused_before_any_launch(V):
         assert attn(chunk=C.byref(big), le=1, ws=4096, n=need.value - 1) == cap
         assert attn(chunk=C.byref(big), le=1, ws=4100, n=need.value) == inv
     assert lib.vlc_pages_clear(None, None) == inv and lib.vlc_pages_status(None, None) == inv
+    # valid calls, but the arena's status and counters have not been cleared
+    small = C.byref(chunk_of(V, max_len=16, max_new=1))
+    for st in (write(), read(), attn(chunk=small), lib.vlc_pages_status(h, None)):
+        assert st == inv and "vlc_pages_clear" in V.vlc_last_error_string()
     lib.vlc_pages_destroy(h)
 
 
