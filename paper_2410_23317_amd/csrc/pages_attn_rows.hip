@@ -127,11 +127,12 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void pages_rows_kernel(P
                 qf[rb][ks] = __builtin_bit_cast(bf16x8_t, w);
             }
     }
-    float m[RB], z[RB], peak[RB];      // what the weights are relative to, their sum, the largest logit; exponent domain
+    // what the weights are relative to, their sum, the largest logit, and how far a logit may lie above m (exponent domain)
+    float m[RB], z[RB], peak[RB], slack[RB];
     f32x16_t o[RB][DT];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        m[rb] = peak[rb] = kNoMax; z[rb] = 0.f;
+        m[rb] = z[rb] = 0.f; peak[rb] = slack[rb] = kNoMax;          // any logit sets the first m
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[rb][dt] = f32x16_t{0};
     }
@@ -250,9 +251,9 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void pages_rows_kernel(P
             f[4 * q4] = x.x; f[4 * q4 + 1] = x.y; f[4 * q4 + 2] = x.z; f[4 * q4 + 3] = x.w;
         }
     };
-    // Codes: the logits in the exponent domain.  Masked: keys that a row does not see.  Returns whether a running maximum has to
-    // be raised.
-    float top[RB];                     // largest logit of the step, exponent domain
+    // The products become logits in the exponent domain, relative to m (codes: times the key's scale).  Masked: keys that a row
+    // does not see.  Returns whether m has to be raised.
+    float top[RB];                     // largest of the step
     auto finish_logits = [&](auto masked, int j, f32x16_t (&acc)[RB]) {
         constexpr bool MASKED = decltype(masked)::value;
         float f[16];
@@ -262,24 +263,28 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void pages_rows_kernel(P
         for (int rb = 0; rb < RB; ++rb) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                if constexpr (Q8) acc[rb][i] *= f[i];
+                acc[rb][i] = fmaf(acc[rb][i], Q8 ? f[i] : c, -m[rb]);
                 if constexpr (MASKED) acc[rb][i] = 32 * j + acc_row(i, lane) <= last[rb] ? acc[rb][i] : -INFINITY;
             }
             float t = acc[rb][0];
 #pragma unroll
             for (int i = 1; i < 16; ++i) t = fmaxf(t, acc[rb][i]);
-            top[rb] = Q8 ? t : t * c;
-            peak[rb] = fmaxf(peak[rb], top[rb]);
-            raise |= top[rb] > m[rb] + kSlack;
+            top[rb] = t;
+            peak[rb] = fmaxf(peak[rb], t + m[rb]);
+            raise |= t > slack[rb];
         }
         return __any(raise) != 0;
     };
-    auto raise_max = [&]() {
+    auto raise_max = [&](f32x16_t (&s)[RB]) {
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-            const float m_new = fmaxf(m[rb], max_across_halves(top[rb])), corr = exp2_fast(m[rb] - m_new);
-            m[rb] = m_new;
+            const float t = max_across_halves(top[rb]);
+            const bool first = slack[rb] < 0.f;
+            const float by = t > 0.f || (first && t > -INFINITY) ? t : 0.f, corr = first ? 1.f : exp2_fast(-by);
+            if (t > -INFINITY) slack[rb] = kSlack;
+            m[rb] += by;
             z[rb] *= corr;
+            s[rb] -= by;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) o[rb][dt] *= corr;
         }
@@ -297,7 +302,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void pages_rows_kernel(P
             float zs[2] = {0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const float p = exp2_fast(Q8 ? s[rb][i] - m[rb] : fmaf(s[rb][i], c, -m[rb]));
+                const float p = exp2_fast(s[rb][i]);
                 zs[i & 1] += p;
                 float w = p;
                 if constexpr (Q8) {
@@ -370,7 +375,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void pages_rows_kernel(P
         load_k(j);
         products(s);
         load_k(j + 1);
-        if (finish_logits(yes, j, s)) raise_max();
+        if (finish_logits(yes, j, s)) raise_max(s);
         // Steps up to jstop.  Raising the maximum stands outside the loop over the steps: inside, the accumulators would have two
         // definitions to choose from, and be copied at every step.
         auto run = [&](auto masked, int jstop) {
@@ -387,7 +392,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void pages_rows_kernel(P
                     raise = step(masked, no, j, s);
                     ++j;
                 } while (!raise && j < jstop);
-                if (raise) raise_max();
+                if (raise) raise_max(s);
             }
         };
         run(no, min(2 * st1, 2 * st_masked) - 2);               // these steps, and what they look ahead to, are seen by all rows
@@ -403,7 +408,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void pages_rows_kernel(P
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
         const int first = r0 + 32 * (RB * wave + rb), r = first + (lane & 31);
-        const float top_m = max_across_halves(peak[rb]), to_top = exp2_fast(m[rb] - top_m);    // relative to the largest logit from here on
+        const float top_m = max_across_halves(peak[rb]), to_top = top_m > kNoMax ? exp2_fast(m[rb] - top_m) : 1.f;     // relative to the largest logit from here on
         const float zt = (z[rb] + __shfl_xor(z[rb], 32, kWave)) * to_top;
         const float factor = a.n_units > 1 ? to_top : zt == 0.f ? 0.f : to_top / zt;
 #pragma unroll
