@@ -407,7 +407,7 @@ __device__ __forceinline__ void store_column(const PagesAttnParams& a, int l, in
 }
 
 template <int D, int FMT, int NT>
-__global__ __launch_bounds__(kThreads, NT == 1 ? 3 : NT == 2 ? 2 : 1) void pages_few_kernel(PagesAttnParams a) {
+__global__ __launch_bounds__(kThreads, NT == 1 ? 3 : NT == 2 || D == 64 ? 2 : 1) void pages_few_kernel(PagesAttnParams a) {
     constexpr bool ONE_LAUNCH = NT == 1;        // the last unit of a row merges; else a second kernel does
     typedef typename PageRow<FMT>::T T;
     typedef FewTile<D, FMT, NT> Tile;
