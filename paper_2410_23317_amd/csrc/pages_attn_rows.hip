@@ -25,7 +25,6 @@ namespace {
 
 using tiles::acc_row;
 
-constexpr int kWaves = 4, kThreads = kWaves * 64;
 constexpr int kStage = 64;             // keys per stage
 constexpr int kRing = 4;
 constexpr float kSlack = 10.f;
@@ -53,8 +52,9 @@ __device__ __forceinline__ float max_across_halves(float x) {
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-template <int D, int FMT, int RB>
-__global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void pages_rows_kernel(PagesRowsParams ra) {
+template <int D, int FMT, int RB, int W>
+__global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams ra) {
+    constexpr int kWaves = W, kThreads = W * 64, kRows = 32 * RB * W;
     constexpr bool Q8 = PageRow<FMT>::kQuantised;
     constexpr int KS = D / 16, DT = D / 32, PPR = D / 8;       // k-steps of K Q^T, 32-wide tiles of d, pieces per row
     constexpr int ROWB = D * PageRow<FMT>::kElemBytes;         // bytes of a row in a page
@@ -80,10 +80,10 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void pages_rows_kernel(P
     const ChunkLen len = chunk_len(a.p, b);
     if (!len.ok && l == 0 && h == 0 && inner == 0 && tid == 0) report_lens(a.p, b);
     const int g = a.p.g, rows = g * len.c, first_new = len.n - len.c;
-    const int r0 = rblk * (128 * RB);                          // the block's rows: r0 + 32 RB wave + 32 rb + lane % 32
+    const int r0 = rblk * kRows;                          // the block's rows: r0 + 32 RB wave + 32 rb + lane % 32
     if (r0 >= rows) return;
     const int first_last = first_new + r0 / g;                 // last key of the block's first row, and of its last row
-    const int last_last = first_new + (min(r0 + 128 * RB, rows) - 1) / g;
+    const int last_last = first_new + (min(r0 + kRows, rows) - 1) / g;
     const int st0 = split * ra.steps_per_split, st1 = min(last_last / kStage + 1, st0 + ra.steps_per_split);
     const int st_masked = (first_last + 1) / kStage;           // first stage that some row does not see to its end
 
@@ -403,8 +403,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void pages_rows_kernel(P
     const int64_t prow0 = ((int64_t)group * a.n_units + split) * ((int64_t)g * a.p.max_new);
     // Through LDS, so that memory sees whole rows: a lane holds 4 neighbouring numbers of d at a time, the wave 32 rows of them.
     constexpr int PIECES = D / 4;                              // 16-byte pieces of a row of fp32 numbers
-    f32x4_t* sO = reinterpret_cast<f32x4_t*>(wave < 2 ? &sK[0][0] : &sV[0][0]) + (wave & 1) * (32 * PIECES);
-    static_assert(sizeof(sK) >= 2 * 32 * PIECES * 16, "two waves' rows in each half of the ring");
+    f32x4_t* sO = reinterpret_cast<f32x4_t*>(wave < W / 2 ? &sK[0][0] : &sV[0][0]) + wave % (W / 2) * (32 * PIECES);
+    static_assert(sizeof(sK) >= W / 2 * 32 * PIECES * 16, "the rows of half the waves in each half of the ring");
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
         const int first = r0 + 32 * (RB * wave + rb), r = first + (lane & 31);
@@ -446,7 +446,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void pages_rows_kernel(P
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         const int t0 = sBad[0] * kStage, t1 = sBad[1] * kStage + kStage - 1;
-        for (int x = tid; x < min(128 * RB, rows - r0) * D; x += kThreads) {
+        for (int x = tid; x < min(kRows, rows - r0) * D; x += kThreads) {
             const int r = r0 + x / D, d = x % D;
             float add = 0.f;
             bool any = false;
@@ -502,8 +502,9 @@ RowsPlan plan(const PagesCall& c) {
 template <int D, int FMT>
 void launch(const PagesRowsParams& ra, int rb, hipStream_t st) {
     const unsigned grid = (unsigned)ra.groups * ra.row_blocks * ra.a.n_units;
-    if (rb == 1) pages_rows_kernel<D, FMT, 1><<<grid, kThreads, 0, st>>>(ra);
-    else pages_rows_kernel<D, FMT, 2><<<grid, kThreads, 0, st>>>(ra);
+    if (rb == 1) pages_rows_kernel<D, FMT, 1, 4><<<grid, 256, 0, st>>>(ra);
+    else if constexpr (D == 128) pages_rows_kernel<D, FMT, 1, 8><<<grid, 512, 0, st>>>(ra);
+    else pages_rows_kernel<D, FMT, 2, 4><<<grid, 256, 0, st>>>(ra);
     if (ra.a.n_units > 1) launch_pages_rows_merge<bf16_t, D>(ra, st);
 }
 
