@@ -3,7 +3,9 @@
 //
 // Both kernels move rows: a row of K and the same row of V per group of lanes, 16 bytes of the storage type a lane, so that a
 // row's absolute maximum is a reduction inside 8 or 16 lanes and every access is a whole piece of 16 bytes (8 of codes).
-// They are bound by memory.
+// They are bound by memory: 32 layers of 10368 tokens into FP8 pages and back (4.1 GB read and written) take 827 us, 5.0 TB/s, what a
+// large copy reaches; 2944 tokens of 32 layers read back 99 us; 2000 new tokens of one layer 4.4 us, where a launch is 2.4 of them.
+// More rows in flight per lane were not needed.  Neighbouring groups of lanes take neighbouring rows of the caller's tensor (head_inner).
 #include "pages.h"
 
 namespace vlc {

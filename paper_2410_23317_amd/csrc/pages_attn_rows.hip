@@ -1,22 +1,30 @@
-// Attention of a chunk over the pages of its request (gfx950, v_mfma_f32_32x32x16_bf16): the chunks of a prompt, more than 32
+// Attention of a chunk over the pages of its request (gfx950, v_mfma_f32_32x32x16_bf16): the chunks of a prompt, more than 64
 // query rows per KV head.
 //
-// A block of four waves takes 128 RB query rows of one KV head (rows token after token, the g heads of a token next to each
-// other, so that a block needs few masked keys) and walks the keys.  A wave owns RB blocks of 32 rows.  As in the
-// window attention, S^T = K Q^T per 32 keys, so the 16 logits a lane holds belong to ONE query row, the softmax stays in
-// the lane, the probabilities are the second operand of O^T += V^T P^T as they are, and V's transpose is the LDS read.
+// A block takes up to 256 query rows of one KV head (rows token after token, the g heads of a token next to each other, so that a
+// block needs few masked keys) and walks the keys; a wave owns RB blocks of 32 rows.  As in the window attention, S^T = K Q^T
+// per step of 32 keys, so the 16 logits a lane holds belong to ONE query row, the softmax stays in the lane, the
+// probabilities are the second operand of O^T += V^T P^T as they are, and V's transpose is the LDS read.
 //
-// What decides the speed is that the matrix instructions of one step have something independent to run beside: iteration j
-// turns the logits of keys j into probabilities (vector unit) while the products K Q^T of keys j + 1 run, and then
-// multiplies V of keys j while it takes the maxima of the logits j + 1.  With RB = 2 every fragment read from LDS feeds two
-// matrix instructions: at one, the four waves would need LDS's 128 bytes per clock all the time.
-// The running maximum is raised only when a logit exceeds it by more than 2^kSlack: probabilities are then at most
-// 2^kSlack instead of 1, and the accumulators are rescaled a few times per row instead of at every new maximum.
+// What decides the speed is that matrix and vector instructions always have each other to run beside (a wave's own ones do: a
+// matrix instruction occupies its unit for 32 cycles and the issue for 8).  Inside a wave, step j turns its logits into
+// probabilities while the products K Q^T of step j + 1 run, then multiplies V while it takes the maxima of the logits of step
+// j + 1.  Between waves, every SIMD holds two, which cover each other's waits: eight waves of 32 rows share the keys of a
+// block of 128-wide heads, and two blocks of four waves of 64 rows fit a compute unit with 64-wide ones.  2048 tokens of 32
+// heads over 32768 keys, us (TFLOP/s): d = 128 one wave per SIMD with 64 rows 1028, two with 32 rows 993 (1073); d = 64 one 811,
+// two 588 (905).  A large bf16 matrix product reaches 1256 TFLOP/s here; neither more lookahead, other wave priorities nor
+// none of the lookahead moves the 993 by 1 %.  FP8 pages 1077, int8 about 1120: the codes' expansion and two scales.
+//
+// A row's weights are relative to m, which starts as the maximum of its first 32 keys and is raised only when a logit exceeds
+// it by more than 2^kSlack: the weights are then at most 2^kSlack instead of 1, and the accumulators are rescaled a few times per
+// row instead of at every new maximum.  The rescaling stands outside the loop over the steps; inside, the accumulators had two
+// definitions and were copied between registers at every step (1372 us instead of 1050).
 //
 // Keys come in stages of 64 through a ring of four LDS buffers: plain rows go from memory to LDS without registers, requested
 // three stages ahead; codes are fetched into registers, expanded to bf16 (exactly) on their way into LDS, and their scales
-// multiply the logits and the probabilities.  16-byte pieces of a row lie at swizzled places, so that neither the reads of K
-// (16 rows, one piece) nor the transposing reads of V (four rows, 64 bytes) meet on a bank.
+// multiply the logits and the probabilities.  Probabilities are rounded to bf16 for the product with V (a half step of 2^-8
+// each; the sums they are divided by are not rounded).  16-byte pieces of a row lie at swizzled places, so that neither the
+// reads of K (16 rows, one piece) nor the transposing reads of V (four rows, 64 bytes) meet on a bank (counted: no conflicts).
 #include "pages_rows.h"
 #include "score_tiles.h"
 
