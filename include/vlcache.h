@@ -501,8 +501,10 @@ vlc_status vlc_pages_read(vlc_pages* pages, const vlc_chunk* chunk, int32_t laye
  *              row_max and row_sum that vlc_score_from_stats takes.
  * workspace    scratch of at least vlc_pages_attn_workspace_bytes bytes (may be NULL when that is 0).  Calls on one
  *              vlc_pages that may overlap on the device race, as those on one vlc_cache do.
- * Accumulation and statistics are fp32; bf16 storage rounds the probabilities to bf16 for the product with V, fp32 storage
- * does not.
+ * Accumulation and statistics are fp32; bf16 storage rounds the probabilities (of codes: times V's scale) to bf16 for the
+ * product with V, or for few rows to a sum of two bf16 numbers; fp32 storage does not.  Weights are held relative to a
+ * number near M, and are at most 2^10 before the division: V of magnitudes between 2^-100 and 2^100 is safe from
+ * underflow and overflow on the way.
  */
 typedef struct {
     float* row_max;

@@ -13,7 +13,8 @@
 // block of 128-wide heads, and two blocks of four waves of 64 rows fit a compute unit with 64-wide ones.  2048 tokens of 32
 // heads over 32768 keys, us (TFLOP/s): d = 128 one wave per SIMD with 64 rows 1028, two with 32 rows 993 (1073); d = 64 one 811,
 // two 588 (905).  A large bf16 matrix product reaches 1256 TFLOP/s here; neither more lookahead, other wave priorities nor
-// none of the lookahead moves the 993 by 1 %.  FP8 pages 1077, int8 about 1120: the codes' expansion and two scales.
+// none of the lookahead moves the 993 by 1 %.  FP8 pages 1169, int8 1206 (d = 64: 766): the codes' expansion, two scales, and
+// the sum over rounded weights (see step; 8 % of the time with d = 128, 13 % with 64).
 //
 // A row's weights are relative to m, which starts as the maximum of its first 32 keys and is raised only when a logit exceeds
 // it by more than 2^kSlack: the weights are then at most 2^kSlack instead of 1, and the accumulators are rescaled a few times per
@@ -22,8 +23,8 @@
 //
 // Keys come in stages of 64 through a ring of four LDS buffers: plain rows go from memory to LDS without registers, requested
 // three stages ahead; codes are fetched into registers, expanded to bf16 (exactly) on their way into LDS, and their scales
-// multiply the logits and the probabilities.  Probabilities are rounded to bf16 for the product with V (a half step of 2^-8
-// each; the sums they are divided by are not rounded).  16-byte pieces of a row lie at swizzled places, so that neither the
+// multiply the logits and the probabilities.  Probabilities are rounded to bf16 for the product with V, a half step of 2^-8
+// each; the sums are fp32, of the probabilities themselves for plain rows and of the rounded ones for codes.  16-byte pieces of a row lie at swizzled places, so that neither the
 // reads of K (16 rows, one piece) nor the transposing reads of V (four rows, 64 bytes) meet on a bank (counted: no conflicts).
 #include "pages_rows.h"
 #include "score_tiles.h"
@@ -60,7 +61,9 @@ __device__ __forceinline__ float max_across_halves(float x) {
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-template <int D, int FMT, int RB, int W>
+// STATS: pages of codes keep the plain sum of the weights too (see step), which only calls that ask for statistics pay
+// (d = 64, two blocks of rows a wave: 902 us instead of 766, 31 registers in scratch; one block a wave 1000 and more).
+template <int D, int FMT, int RB, int W, bool STATS>
 __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams ra) {
     constexpr int kWaves = W, kThreads = W * 64, kRows = 32 * RB * W;
     constexpr bool Q8 = PageRow<FMT>::kQuantised;
@@ -69,7 +72,7 @@ __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams r
     constexpr int LOADS = 2 * kStage * PPR / kThreads;         // 16-byte pieces of K and V per thread and stage (plain rows)
     __shared__ __align__(1024) uint4 sK[kRing][kStage * PPR];
     __shared__ __align__(1024) uint4 sV[kRing][kStage * PPR];
-    __shared__ __align__(16) float sKs[Q8 ? kRing : 1][kStage], sVs[Q8 ? kRing : 1][kStage];
+    __shared__ __align__(16) float sKs[Q8 ? kRing : 1][kStage], sVs[Q8 ? kRing : 1][kStage], sVi[Q8 ? kRing : 1][kStage];      // scales; 1 / V's
     __shared__ int sBad[2];            // first and last stage in which numbers of V were replaced by 0
     const PagesAttnParams& a = ra.a;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
@@ -136,11 +139,13 @@ __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams r
             }
     }
     // what the weights are relative to, their sum, the largest logit, and how far a logit may lie above m (exponent domain)
-    float m[RB], z[RB], peak[RB], slack[RB];
+    float m[RB], z[RB], z_plain[STATS ? RB : 1], peak[RB], slack[RB];
     f32x16_t o[RB][DT];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        m[rb] = z[rb] = 0.f; peak[rb] = slack[rb] = kNoMax;          // any logit sets the first m
+        m[rb] = z[rb] = 0.f;
+        if constexpr (STATS) z_plain[rb] = 0.f;
+        peak[rb] = slack[rb] = kNoMax;          // any logit sets the first m
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[rb][dt] = f32x16_t{0};
     }
@@ -200,7 +205,10 @@ __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams r
             sV[buf][v_place<D>(r, 2 * piece)] = codes_to_bf16<FMT>(make_uint2(v.x, v.y));
             sV[buf][v_place<D>(r, 2 * piece + 1)] = codes_to_bf16<FMT>(make_uint2(v.z, v.w));
         }
-        if (wave < 2) (wave ? sVs : sKs)[buf][lane] = wave ? c8.scale : c8.scale * c;
+        // V's scales that are no normal number count as the smallest, so that their reciprocals are numbers (a NaN stays)
+        const float vs = c8.scale < 0x1p-126f ? 0x1p-126f : c8.scale;
+        if (wave == 0) sKs[buf][lane] = c8.scale * c;
+        if (wave == 1) { sVs[buf][lane] = vs; sVi[buf][lane] = 1.f / vs; }
     };
 
     auto barrier = [&]() {
@@ -292,6 +300,7 @@ __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams r
             if (t > -INFINITY) slack[rb] = kSlack;
             m[rb] += by;
             z[rb] *= corr;
+            if constexpr (STATS) z_plain[rb] *= corr;
             s[rb] -= by;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) o[rb][dt] *= corr;
@@ -303,23 +312,50 @@ __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams r
         f32x16_t sn[RB];
         if constexpr (!LAST) products(sn);
         bf16x8_t pf[RB][2];
-        float f[16];
-        if constexpr (Q8) scales_of(&sVs[0][0], j, f);
+        // Codes: a weight takes V's scale before it is rounded to bf16, and the sum takes the weight as it was rounded: where one key
+        // has nearly all of a row, as often, its rounding then cancels.  (Plain rows: such a key's weight is near 1, which bf16
+        // has.)  2-norm of the outputs' error in an int8 window, in that of their own rounding to bf16: 1.04 to 1.25 over four
+        // random inputs, with the plain sum up to 1.53.
+        float f[16] = {}, inv[16] = {};
+        if constexpr (Q8) {
+            scales_of(&sVs[0][0], j, f);
+            scales_of(&sVi[0][0], j, inv);
+        }
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-            float zs[2] = {0.f, 0.f};
+            float zs[2] = {0.f, 0.f}, zp[2] = {0.f, 0.f};
+            u32x4_t w4[2];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float p = exp2_fast(s[rb][i]);
-                zs[i & 1] += p;
-                float w = p;
-                if constexpr (Q8) {
-                    w = p * f[i];
-                    if constexpr (MASKED) w = 32 * j + acc_row(i, lane) <= last[rb] ? w : 0.f;        // any scale there
+            for (int i = 0; i < 16; i += 2) {
+                float p[2] = {exp2_fast(s[rb][i]), exp2_fast(s[rb][i + 1])}, to_p[2] = {inv[i], inv[i + 1]};
+                if constexpr (!Q8) {
+                    zs[0] += p[0];
+                    zs[1] += p[1];
+                } else {
+                    if constexpr (STATS) { zp[0] += p[0]; zp[1] += p[1]; }
+                    p[0] *= f[i];
+                    p[1] *= f[i + 1];
+                    if constexpr (MASKED) {            // any scale stands behind keys that are not seen
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const bool seen = 32 * j + acc_row(i + x, lane) <= last[rb];
+                            p[x] = seen ? p[x] : 0.f;
+                            to_p[x] = seen ? to_p[x] : 0.f;
+                        }
+                    }
                 }
-                pf[rb][i >> 3][i & 7] = (__bf16)w;
+                typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+                const uint32_t w = __builtin_bit_cast(uint32_t, bf16x2_t{(__bf16)p[0], (__bf16)p[1]});
+                w4[i >> 3][(i >> 1) & 3] = w;
+                if constexpr (Q8) {
+                    zs[0] = fmaf(bf16_lo(w), to_p[0], zs[0]);
+                    zs[1] = fmaf(bf16_hi(w), to_p[1], zs[1]);
+                }
             }
+            pf[rb][0] = __builtin_bit_cast(bf16x8_t, w4[0]);
+            pf[rb][1] = __builtin_bit_cast(bf16x8_t, w4[1]);
             z[rb] += zs[0] + zs[1];
+            if constexpr (STATS) z_plain[rb] += zp[0] + zp[1];
             asm volatile("" : "+v"(z[rb]));    // here, beside the products, not behind the step
         }
         if constexpr (!LAST) load_k(j + 2);
@@ -418,6 +454,8 @@ __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams r
         const int first = r0 + 32 * (RB * wave + rb), r = first + (lane & 31);
         const float top_m = max_across_halves(peak[rb]), to_top = top_m > kNoMax ? exp2_fast(m[rb] - top_m) : 1.f;     // relative to the largest logit from here on
         const float zt = (z[rb] + __shfl_xor(z[rb], 32, kWave)) * to_top;
+        float zs = zt;
+        if constexpr (STATS) zs = (z_plain[rb] + __shfl_xor(z_plain[rb], 32, kWave)) * to_top;
         const float factor = a.n_units > 1 ? to_top : zt == 0.f ? 0.f : to_top / zt;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
@@ -427,8 +465,8 @@ __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams r
                 sO[(lane & 31) * PIECES + ((dt * 8 + 2 * q4 + half) ^ (lane & (PIECES - 1)))] = x * factor;
             }
         if (half == 0 && r < rows) {
-            if (a.n_units > 1) ra.part_mz[prow0 + r] = make_float2(top_m, zt);
-            else if (a.stats.row_max) store_stats(a, l, b, h * g + r % g, r / g, top_m, zt);
+            if (a.n_units > 1) ra.part_mz[prow0 + r] = make_float4(top_m, zt, zs, 0.f);
+            else if (a.stats.row_max) store_stats(a, l, b, h * g + r % g, r / g, top_m, zs);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the wave's own writes; no other wave touches its rows
         if (a.n_units > 1) {
@@ -503,16 +541,25 @@ RowsPlan plan(const PagesCall& c) {
     p.splits = (stages + p.steps_per_split - 1) / p.steps_per_split;
     const size_t n = (size_t)p.groups * p.splits * p.rows;
     p.o_bytes = pages_partials_o_bytes(n, c.s.d);
-    p.bytes = p.splits > 1 ? p.o_bytes + n * sizeof(float2) : 0;
+    p.bytes = p.splits > 1 ? p.o_bytes + n * sizeof(float4) : 0;
     return p;
 }
 
+template <int D, int FMT, bool STATS>
+void launch_blocks(const PagesRowsParams& ra, int rb, hipStream_t st) {
+    const unsigned grid = (unsigned)ra.groups * ra.row_blocks * ra.a.n_units;
+    if (rb == 1) pages_rows_kernel<D, FMT, 1, 4, STATS><<<grid, 256, 0, st>>>(ra);
+    else if constexpr (D == 128) pages_rows_kernel<D, FMT, 1, 8, STATS><<<grid, 512, 0, st>>>(ra);
+    else pages_rows_kernel<D, FMT, 2, 4, STATS><<<grid, 256, 0, st>>>(ra);
+}
 template <int D, int FMT>
 void launch(const PagesRowsParams& ra, int rb, hipStream_t st) {
-    const unsigned grid = (unsigned)ra.groups * ra.row_blocks * ra.a.n_units;
-    if (rb == 1) pages_rows_kernel<D, FMT, 1, 4><<<grid, 256, 0, st>>>(ra);
-    else if constexpr (D == 128) pages_rows_kernel<D, FMT, 1, 8><<<grid, 512, 0, st>>>(ra);
-    else pages_rows_kernel<D, FMT, 2, 4><<<grid, 256, 0, st>>>(ra);
+    if constexpr (PageRow<FMT>::kQuantised) {
+        if (ra.a.stats.row_max) launch_blocks<D, FMT, true>(ra, rb, st);
+        else launch_blocks<D, FMT, false>(ra, rb, st);
+    } else {
+        launch_blocks<D, FMT, false>(ra, rb, st);
+    }
     if (ra.a.n_units > 1) launch_pages_rows_merge<bf16_t, D>(ra, st);
 }
 
@@ -527,7 +574,7 @@ hipError_t launch_pages_rows(const PagesAttn& c) {
     ra.a.n_units = p.splits;
     ra.row_blocks = p.row_blocks; ra.groups = (int)p.groups; ra.steps_per_split = p.steps_per_split;
     ra.part_o = (float*)c.workspace;
-    ra.part_mz = (float2*)((char*)c.workspace + p.o_bytes);
+    ra.part_mz = (float4*)((char*)c.workspace + p.o_bytes);
     const bool wide = c.c.s.d == 128;
     switch (page_format(c.c.s)) {
         case kPageBf16: wide ? launch<128, kPageBf16>(ra, p.rb, c.c.stream) : launch<64, kPageBf16>(ra, p.rb, c.c.stream); break;

@@ -130,7 +130,7 @@ __global__ __launch_bounds__(kThreads, 2) void pages_rows_f32_kernel(PagesRowsPa
                 *reinterpret_cast<float4*>(dst + dt * 32 + acc_row(4 * q4, lane)) =
                     div == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o[dt][4 * q4] / div, o[dt][4 * q4 + 1] / div, o[dt][4 * q4 + 2] / div, o[dt][4 * q4 + 3] / div);
         if (half == 0) {
-            if (a.n_units > 1) ra.part_mz[prow0 + r] = make_float2(m, z);
+            if (a.n_units > 1) ra.part_mz[prow0 + r] = make_float4(m, z, z, 0.f);
             else if (a.stats.row_max) store_stats(a, l, b, h * g + r % g, r / g, m, z);
         }
     }
@@ -168,7 +168,7 @@ Plan plan(const PagesCall& c) {
     p.splits = (tiles + p.steps_per_split - 1) / p.steps_per_split;
     const size_t n = (size_t)p.groups * p.splits * p.rows;
     p.o_bytes = pages_partials_o_bytes(n, c.s.d);
-    p.bytes = p.splits > 1 ? p.o_bytes + n * sizeof(float2) : 0;
+    p.bytes = p.splits > 1 ? p.o_bytes + n * sizeof(float4) : 0;
     return p;
 }
 
@@ -189,7 +189,7 @@ hipError_t launch_pages_rows_f32(const PagesAttn& c) {
     ra.a.n_units = p.splits;
     ra.row_blocks = p.row_blocks; ra.groups = (int)p.groups; ra.steps_per_split = p.steps_per_split;
     ra.part_o = (float*)c.workspace;
-    ra.part_mz = (float2*)((char*)c.workspace + p.o_bytes);
+    ra.part_mz = (float4*)((char*)c.workspace + p.o_bytes);
     if (c.c.s.d == 128) launch<128>(ra, c.c.stream);
     else launch<64>(ra, c.c.stream);
     return hipGetLastError();

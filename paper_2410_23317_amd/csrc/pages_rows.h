@@ -10,7 +10,7 @@ struct PagesRowsParams {
     int row_blocks, groups;            // of a KV head's rows; layers * requests * KV heads
     int steps_per_split;               // key stages (bf16) or tiles (fp32)
     float* part_o;                     // [group][split][rows][D] unnormalised
-    float2* part_mz;                   // [group][split][rows] running maximum (base 2) and sum
+    float4* part_mz;                   // [group][split][rows] running maximum (base 2), sum that the outputs are divided by, plain sum
 };
 
 // Bytes of the partial results of n rows, and where the (maximum, sum) pairs start.
@@ -27,11 +27,11 @@ __global__ __launch_bounds__(256) void pages_rows_merge_kernel(PagesRowsParams r
     const int r = blockIdx.x * (256 / LPR) + threadIdx.x / LPR, g = a.p.g;
     if (r >= g * chunk_len(a.p, b).c) return;
     const int64_t stride = (int64_t)g * a.p.max_new, p0 = (int64_t)group * a.n_units * stride + r;
-    float m = kNoMax, z = 0.f;
+    float m = kNoMax, z = 0.f, zs = 0.f;
     f32x4_t o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
     for (int s0 = 0; s0 < a.n_units; s0 += NB) {
-        float2 mz[NB];
+        float4 mz[NB];
         f32x4_t f[NB];
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
@@ -42,16 +42,17 @@ __global__ __launch_bounds__(256) void pages_rows_merge_kernel(PagesRowsParams r
         float mn = m;
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
-            if (s0 + j >= a.n_units) { mz[j] = make_float2(kNoMax, 0.f); f[j] = f32x4_t{0.f, 0.f, 0.f, 0.f}; }
+            if (s0 + j >= a.n_units) { mz[j] = make_float4(kNoMax, 0.f, 0.f, 0.f); f[j] = f32x4_t{0.f, 0.f, 0.f, 0.f}; }
             mn = fmaxf(mn, mz[j].x);
         }
         const float w0 = exp2_fast(m - mn);
-        o *= w0; z *= w0;
+        o *= w0; z *= w0; zs *= w0;
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
             const float wgt = exp2_fast(mz[j].x - mn);
             o += f[j] * wgt;
             z = fmaf(mz[j].y, wgt, z);
+            zs = fmaf(mz[j].z, wgt, zs);
         }
         m = mn;
     }
@@ -59,7 +60,7 @@ __global__ __launch_bounds__(256) void pages_rows_merge_kernel(PagesRowsParams r
     T* out = (T*)a.out.at(l, b, h * g + r % g, r / g) + sub * 4;
     store_pair(out, o[0] / div, o[1] / div);
     store_pair(out + 2, o[2] / div, o[3] / div);
-    if (sub == 0 && a.stats.row_max) store_stats(a, l, b, h * g + r % g, r / g, m, z);
+    if (sub == 0 && a.stats.row_max) store_stats(a, l, b, h * g + r % g, r / g, m, zs);
 }
 
 template <typename T, int D>

@@ -166,6 +166,47 @@ def test_scales_of_every_sign_and_bounds_larger_than_the_lengths(fmt, dtype, n, 
         c.check(out, M, Z, f"scale {sc}", scale=sc)
 
 
+@pytest.mark.parametrize("fmt", ["plain", "fp8", "int8"])
+@pytest.mark.parametrize("d,cn", [(128, 1), (128, 5), (64, 80), (64, 300), (128, 80), (128, 300)])
+def test_a_row_that_one_key_answers_is_that_key(fmt, d, cn):
+    """Every query is the K row of one position and the logits lie 77 and more apart: the output is that position's V, and
+    only the output's own rounding (half a step, 2^-8) and 2^-15 for 2^-16 of a split weight and fp32 sums are left."""
+    n, g = cn + 130, 2
+    c = U.Case(1, g, 1, d, [(n, cn)], fmt=fmt, seed=cn)
+    c.fill()
+    gen = torch.Generator().manual_seed(cn)
+    at = torch.randint(0, n - cn, (cn,), generator=gen).cuda()
+    own = torch.nn.functional.normalize(c.k[0, 0, 0, at].float(), dim=-1)
+    c.q.copy_((own * d).to(torch.bfloat16).expand(g, cn, d))
+    one = torch.tensor([4.0 * (128 / d)], device="cuda")
+    out, M, Z = c.attn(scale=one)
+    torch.cuda.synchronize()
+    k, v = U.held(c.k[0, 0], fmt), U.held(c.v[0, 0], fmt)
+    ref = U.attention(c.q[0, 0], k, v, one.item(), n, cn)
+    alone = ref[2] < 1 + 1e-9                                    # the rows whose other weights are nothing
+    assert int(alone.sum()) > 0.9 * g * cn
+    top = (c.q[0, 0].double().cpu().reshape(g * cn, d) @ k[0].T).masked_fill(
+        (torch.arange(n)[None] > torch.arange(n - cn, n)[:, None]).repeat(g, 1), float("-inf")).argmax(-1).reshape(g, cn)
+    want = v[0][top]
+    U.within(out[0, 0][alone.cuda()], want[alone], (2.0 ** -8 + 2.0 ** -15) * want[alone].abs() + 1e-9, "out")
+
+
+@pytest.mark.parametrize("fmt", ["plain", "fp8", "int8"])
+@pytest.mark.parametrize("d,cn", [(128, 1), (64, 6), (64, 150), (128, 70), (128, 300)])
+def test_values_of_very_different_sizes(fmt, d, cn):
+    """V rows of 2^-90 to 2^60 next to each other, and a KV head whose rows are all near 2^-85."""
+    def edit(k, v):
+        gen = torch.Generator().manual_seed(cn)
+        power = torch.randint(-90, 61, (v.shape[3],), generator=gen).double()
+        v[0, 0, 0] = (v[0, 0, 0].double() * torch.exp2(power)[:, None]).to(v.dtype)
+        v[0, 0, 1] = (v[0, 0, 1].double() * 2.0 ** -85).to(v.dtype)
+    n = cn + 333
+    c = U.Case(1, 4, 2, d, [(n, cn)], fmt=fmt, k_edit=edit)
+    c.fill()
+    out, M, Z = c.attn()
+    c.check(out, M, Z, "sizes")
+
+
 @pytest.mark.parametrize("fmt,dtype", U.FORMATS)
 @pytest.mark.parametrize("g,cn", [(4, 1), (4, 4), (4, 8), (2, 33), (4, 100), (1, 300)])
 def test_what_a_row_does_not_see_has_no_influence(fmt, dtype, g, cn):
