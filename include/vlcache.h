@@ -461,7 +461,8 @@ typedef struct {
 
 /* Rows of a tensor [layers in range, B, heads, rows, d]: the element strides of the first four, d itself being contiguous.
  * data is 16-byte aligned, the strides are non-negative and multiples of 16 bytes.  K, V [B,L,Hkv,m,d] and what a projection
- * leaves, [B,rows,heads,d] per layer, or a slice of it, are taken as they are.  Outputs must not overlap. */
+ * leaves, [B,rows,heads,d] per layer, or a slice of it, are taken as they are.  Outputs must not overlap each other or
+ * an input. */
 typedef struct {
     void* data;
     int64_t layer, request, head, row;

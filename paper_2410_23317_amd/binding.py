@@ -428,6 +428,9 @@ def make_chunk(table: torch.Tensor, max_new: int, max_len: int, lens: Optional[t
         raise ValueError("lens must be an int32 tensor [B, 2]")
     c = vlc_chunk(table.shape[0], table.shape[1], int(max_new), int(max_len), _ptr(table), _ptr(lens))
     c.tensors = (table, lens)
+    c.device_index = table.get_device()
+    if lens is not None and lens.get_device() != c.device_index:
+        raise ValueError("table and lens must lie on one device")
     return c
 
 
@@ -443,9 +446,11 @@ def _rows(t: Optional[torch.Tensor], name: str, pages: Pages, dims) -> Optional[
     return vlc_rows(t.data_ptr(), layer, request, head, row)
 
 
-def _pages_stream(pages: Pages) -> int:
+def _pages_stream(pages: Pages, chunk: Optional[vlc_chunk] = None) -> int:
     if pages.device_index != torch.cuda.current_device():
         raise ValueError(f"the pages lie on {pages.arena.device}, which is not the current device")
+    if chunk is not None and chunk.device_index != pages.device_index:
+        raise ValueError(f"the chunk's table and lens must lie on {pages.arena.device}")
     return torch._C._cuda_getCurrentRawStream(pages.device_index)
 
 
@@ -457,7 +462,7 @@ def vlc_pages_write(pages: Pages, chunk: vlc_chunk, layer_begin, layer_end, k_ne
     s = pages.shape
     dims = (layer_end - layer_begin, chunk.B, s.Hkv, chunk.max_new, s.d)
     k, v = _rows(k_new, "k_new", pages, dims), _rows(v_new, "v_new", pages, dims)
-    st = lib.vlc_pages_write(pages.handle, chunk, layer_begin, layer_end, _ref(k), _ref(v), _pages_stream(pages))
+    st = lib.vlc_pages_write(pages.handle, chunk, layer_begin, layer_end, _ref(k), _ref(v), _pages_stream(pages, chunk))
     if st:
         _check(st)
 
@@ -469,7 +474,7 @@ def vlc_pages_read(pages: Pages, chunk: vlc_chunk, layer_begin, layer_end, first
     dims = (layer_end - layer_begin, chunk.B, s.Hkv, count, s.d)
     k, v = _rows(k_out, "k_out", pages, dims), _rows(v_out, "v_out", pages, dims)
     _check(lib.vlc_pages_read(pages.handle, C.byref(chunk), int(layer_begin), int(layer_end), int(first), int(count), _ref(k), _ref(v),
-                              _pages_stream(pages)))
+                              _pages_stream(pages, chunk)))
 
 
 def vlc_pages_attn_workspace_bytes(pages: Pages, chunk: vlc_chunk, n_layers) -> int:
@@ -497,9 +502,11 @@ def vlc_pages_attn(pages: Pages, chunk: vlc_chunk, layer_begin, layer_end, q, k_
         stats = vlc_row_stats(row_max.data_ptr(), row_sum.data_ptr(), *row_max.stride()[:3])
     if sm_scale is not None and (sm_scale.dtype is not torch.float32 or sm_scale.numel() < s.L or sm_scale.get_device() != pages.device_index):
         raise ValueError(f"sm_scale must be fp32 of {s.L} numbers on {pages.arena.device}")
+    if workspace is not None and workspace.get_device() != pages.device_index:
+        raise ValueError(f"workspace must lie on {pages.arena.device}")
     qr, o = _rows(q, "q", pages, qd), _rows(out, "out", pages, qd)
     k, v = _rows(k_new, "k_new", pages, kd), _rows(v_new, "v_new", pages, kd)
     st = lib.vlc_pages_attn(pages.handle, chunk, layer_begin, layer_end, _ref(qr), _ref(k), _ref(v), _ptr(sm_scale), _ref(o), _ref(stats),
-                            _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _pages_stream(pages))
+                            _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _pages_stream(pages, chunk))
     if st:
         _check(st)

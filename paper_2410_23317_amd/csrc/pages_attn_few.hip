@@ -8,7 +8,7 @@
 // leave unnormalised partial results.  Up to 16 query rows they store them with device scope and count themselves; the one
 // that counts last merges them and writes the output (its own stores are acknowledged before it counts, so whoever counts last
 // finds all of them in memory).  With more rows one block would read the partial results for longer than a second launch takes
-// (35 rows, eight int8 requests: 30.2 us, by a second kernel 26.0), which then merges.
+// (35 rows, eight int8 requests: 32.2 us, by a second kernel 28.0), which then merges.
 // New rows that the call has to write first are kept in LDS as well: the tiles that hold them take them from there instead of
 // waiting until the stores can be read back.
 //
@@ -223,8 +223,14 @@ struct FewTile {                                // bf16 operands
                     w = p * vsc[j];
                     if (MASKED) w = t0 + 8 * (lane >> 4) + j <= col.last[nt] ? w : 0.f;
                 }
-                pb[nt][j] = (__bf16)w;
-                pl[nt][j] = (__bf16)(w - (float)pb[nt][j]);
+                if constexpr (Q8) {
+                    pb[nt][j] = (__bf16)w;
+                    pl[nt][j] = (__bf16)(w - (float)pb[nt][j]);
+                } else {            // V may hold infinities: both parts of a weight above 0 are above 0, so that their sum is no NaN
+                    const uint32_t first = __float_as_uint(w) & 0xffff0000u;
+                    pb[nt][j] = __builtin_bit_cast(__bf16, (uint16_t)(first >> 16));
+                    pl[nt][j] = (__bf16)__builtin_amdgcn_fmed3f(w - __uint_as_float(first), w, 0x1p-126f);
+                }
             }
         }
         uint32_t v[8][EV / 2];

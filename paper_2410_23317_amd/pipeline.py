@@ -137,6 +137,8 @@ class PagedPrompt:
         max_pages = -(-max_len // page_slots)
         self.max_len = int(max_len)
         if page_table is None:
+            if n_pages is not None and n_pages < B * max_pages:
+                raise ValueError(f"{n_pages} pages are fewer than {max_pages} for each of {B} requests; name shared ones in page_table")
             page_table = torch.arange(B * max_pages, dtype=torch.int32, device=device).view(B, max_pages)
         self.table = page_table
         self.pages = V.vlc_pages_create(V.make_pages_shape(L, Hq, Hkv, d, page_slots, n_pages or B * max_pages, dtype, format), device)
@@ -154,20 +156,33 @@ class PagedPrompt:
         total = [n + c for n, c in zip(self.tokens, new)]
         if max(total) > self.max_len:
             raise ValueError(f"a request would hold {max(total)} tokens, {self.max_len} were provided for")
-        self.tokens = total
         lens = torch.tensor(list(zip(total, new)), dtype=torch.int32).to(self.device)
         self.chunk = V.make_chunk(self.table, max(new), max(total), lens)
+        self.tokens = total
         return self.chunk
+
+    def _used(self, *tensors) -> None:
+        """These own tensors are read on the current stream, which may be another than the one they were made on."""
+        stream = torch.cuda.current_stream(self.device)
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
 
     def extend(self, layer_begin, layer_end, q, k_new, v_new, sm_scale, out, row_max=None, row_sum=None) -> None:
         """The chunk's rows of layers [layer_begin, layer_end) into the pages, and their attention."""
+        if self.chunk is None:
+            raise ValueError("begin_chunk() comes first")
         need = V.vlc_pages_attn_workspace_bytes(self.pages, self.chunk, layer_end - layer_begin)
         if need and (self.workspace is None or self.workspace.numel() < need):
             self.workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+        self._used(self.workspace, self.chunk.tensors[1])
         V.vlc_pages_attn(self.pages, self.chunk, layer_begin, layer_end, q, k_new, v_new, sm_scale, out, row_max, row_sum, self.workspace)
 
     def read(self, k_out, v_out) -> None:
         """Every request's K and V so far, into tensors [B, L, Hkv, m, d]; rows beyond a request's are left as they are."""
+        if self.chunk is None:
+            raise ValueError("begin_chunk() comes first")
+        self._used(self.chunk.tensors[1])
         V.vlc_pages_read(self.pages, self.chunk, 0, self.pages.shape.L, 0, k_out.transpose(0, 1), v_out.transpose(0, 1))
 
     def compress(self, path: VLCachePath, q_win, sm_scale, k_out, v_out) -> None:

@@ -262,6 +262,28 @@ def test_numbers_of_v_that_are_not_finite_and_seen(dtype, cn):
         assert torch.equal(torch.isnan(out[0, 0].cpu()), want)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cn", [1, 3, 6, 8, 17, 80, 300])
+def test_infinities_of_v_that_are_seen(dtype, cn):
+    """They come out as infinities of their sign; two of different signs as NaN."""
+    n, d, inf = cn + 700, 64, float("inf")
+    spots = [(3, 0, inf), (300, 7, -inf), (500, 9, inf), (501, 9, -inf), (699, 30, -inf), (700, 31, inf), (n - 1, 63, -inf)]
+
+    def edit(k, v):
+        for t, e, x in spots:
+            v[0, 0, 1, t, e] = x
+    c = U.Case(1, 8, 2, d, [(n, cn)], ps=16, dtype=dtype, k_edit=edit)
+    c.fill()
+    out, M, Z = c.attn()
+    torch.cuda.synchronize()
+    got = out[0, 0, :, :cn].double().cpu()
+    ref = U.attention(c.q[0, 0, :, :cn], U.held(c.k[0, 0], "plain"), U.held(c.v[0, 0], "plain"), c.scale[0].item(), n, cn)
+    bad = ~torch.isfinite(ref[0])
+    assert torch.equal(torch.nan_to_num(got[bad], 7, inf, -inf), torch.nan_to_num(ref[0][bad], 7, inf, -inf))
+    good = ~bad
+    U.within(got[good], ref[0][good], U.bounds(ref, dtype, d, n)[0][good], "elsewhere")
+
+
 def test_requests_that_share_pages_and_calls_without_lengths():
     """Two requests continue one prompt: its pages stand in both rows of the table; the lengths are the chunk's bounds."""
     import paper_2410_23317_amd as V
@@ -304,6 +326,36 @@ def test_refusals_of_the_binding():
         with pytest.raises(ValueError):
             bad()
     V.vlc_pages_status(c.pages)
+
+
+def test_refusals_of_a_prompt_in_chunks_and_of_another_device():
+    import paper_2410_23317_amd as V
+    from paper_2410_23317_amd import pipeline
+    with pytest.raises(ValueError):
+        pipeline.PagedPrompt(1, 2, 1, 64, torch.bfloat16, 2, 100, page_slots=16, n_pages=13)
+    p = pipeline.PagedPrompt(1, 2, 1, 64, torch.bfloat16, 2, 100, page_slots=16)
+    q, kv, out = (torch.zeros((1, 2, h, 5, 64), dtype=torch.bfloat16, device="cuda") for h in (2, 1, 2))
+    with pytest.raises(ValueError):
+        p.extend(0, 1, q, kv, kv, None, out)
+    with pytest.raises(ValueError):
+        p.read(kv, kv)
+    for new in ([1], [0, 0], [-1, 2], [101, 1]):
+        with pytest.raises(ValueError):
+            p.begin_chunk(new)
+    assert p.tokens == [0, 0]
+    p.begin_chunk([5, 3])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        p.extend(0, 1, q, kv, kv, None, out)
+    torch.cuda.current_stream().wait_stream(side)
+    p.status()
+    assert p.tokens == [5, 3]
+    p.chunk.device_index = 1                                     # as if the table were another device's
+    with pytest.raises(ValueError):
+        p.extend(0, 1, q, kv, kv, None, out)
+    with pytest.raises(ValueError):
+        V.vlc_pages_write(p.pages, p.chunk, 0, 1, kv, kv)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
