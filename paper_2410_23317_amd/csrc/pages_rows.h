@@ -13,7 +13,7 @@ struct PagesRowsParams {
     float4* part_mz;                   // [group][split][rows] running maximum (base 2), sum that the outputs are divided by, plain sum
 };
 
-// Bytes of the partial results of n rows, and where the (maximum, sum) pairs start.
+// Bytes of the partial outputs of n rows, behind which their maxima and sums start.
 inline size_t pages_partials_o_bytes(size_t n, int d) { return (n * d * sizeof(float) + 255) / 256 * 256; }
 
 // Merge of the key splits: D / 4 lanes per row, the loads of NB splits in flight together.  A split beyond what the row's block
