@@ -13,8 +13,8 @@
 // block of 128-wide heads, and two blocks of four waves of 64 rows fit a compute unit with 64-wide ones.  2048 tokens of 32
 // heads over 32768 keys, us (TFLOP/s): d = 128 one wave per SIMD with 64 rows 1028, two with 32 rows 993 (1073); d = 64 one 811,
 // two 588 (905).  A large bf16 matrix product reaches 1256 TFLOP/s here; neither more lookahead, other wave priorities nor
-// none of the lookahead moves the 993 by 1 %.  FP8 pages 1169, int8 1206 (d = 64: 766): the codes' expansion, two scales, and
-// the sum over rounded weights (see step; 8 % of the time with d = 128, 13 % with 64).
+// none of the lookahead moves the 993 by 1 %.  FP8 pages 1159, int8 1192 (d = 64: 781): the codes' expansion, two scales, and
+// the sum over rounded weights (see step; 5 % of the time with d = 128, 13 % with 64).
 //
 // A row's weights are relative to m, which starts as the maximum of its first 32 keys and is raised only when a logit exceeds
 // it by more than 2^kSlack: the weights are then at most 2^kSlack instead of 1, and the accumulators are rescaled a few times per
@@ -61,18 +61,19 @@ __device__ __forceinline__ float max_across_halves(float x) {
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-// STATS: pages of codes keep the plain sum of the weights too (see step), which only calls that ask for statistics pay
-// (d = 64, two blocks of rows a wave: 902 us instead of 766, 31 registers in scratch; one block a wave 1000 and more).
+// STATS: pages of codes keep the plain sum of the weights too, which only calls that ask for statistics pay (d = 64, two blocks of
+// rows a wave: 877 us instead of 781; one block a wave 1000 and more).
 template <int D, int FMT, int RB, int W, bool STATS>
 __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams ra) {
     constexpr int kWaves = W, kThreads = W * 64, kRows = 32 * RB * W;
     constexpr bool Q8 = PageRow<FMT>::kQuantised;
+    constexpr bool ZM = Q8 && (D == 128 || STATS);             // who adds the rounded weights up: the matrix unit, or the vector unit (see step)
     constexpr int KS = D / 16, DT = D / 32, PPR = D / 8;       // k-steps of K Q^T, 32-wide tiles of d, pieces per row
     constexpr int ROWB = D * PageRow<FMT>::kElemBytes;         // bytes of a row in a page
     constexpr int LOADS = 2 * kStage * PPR / kThreads;         // 16-byte pieces of K and V per thread and stage (plain rows)
     __shared__ __align__(1024) uint4 sK[kRing][kStage * PPR];
     __shared__ __align__(1024) uint4 sV[kRing][kStage * PPR];
-    __shared__ __align__(16) float sKs[Q8 ? kRing : 1][kStage], sVs[Q8 ? kRing : 1][kStage], sVi[Q8 ? kRing : 1][kStage];      // scales; 1 / V's
+    __shared__ __align__(16) float sKs[Q8 ? kRing : 1][kStage], sVs[Q8 ? kRing : 1][kStage], sVi[Q8 ? kRing : 1][kStage];      // scales; 1 / V's: fp32, or all first and all second parts
     __shared__ int sBad[2];            // first and last stage in which numbers of V were replaced by 0
     const PagesAttnParams& a = ra.a;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
@@ -139,12 +140,13 @@ __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams r
             }
     }
     // what the weights are relative to, their sum, the largest logit, and how far a logit may lie above m (exponent domain)
-    float m[RB], z[RB], z_plain[STATS ? RB : 1], peak[RB], slack[RB];
+    float m[RB], z[RB], peak[RB], slack[RB];
+    f32x16_t zr[ZM ? RB : 1];          // elements 0 and 1: the sum of the rounded weights over V's scales, in two parts
     f32x16_t o[RB][DT];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
         m[rb] = z[rb] = 0.f;
-        if constexpr (STATS) z_plain[rb] = 0.f;
+        if constexpr (ZM) zr[rb] = f32x16_t{0};
         peak[rb] = slack[rb] = kNoMax;          // any logit sets the first m
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[rb][dt] = f32x16_t{0};
@@ -208,7 +210,18 @@ __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams r
         // V's scales that are no normal number count as the smallest, so that their reciprocals are numbers (a NaN stays)
         const float vs = c8.scale < 0x1p-126f ? 0x1p-126f : c8.scale;
         if (wave == 0) sKs[buf][lane] = c8.scale * c;
-        if (wave == 1) { sVs[buf][lane] = vs; sVi[buf][lane] = 1.f / vs; }
+        if (wave == 1) {
+            const float inv = vs == vs ? 1.f / vs : 0.f;       // of a NaN: where the key is seen, the weight is NaN already
+            sVs[buf][lane] = vs;
+            if constexpr (ZM) {
+                const __bf16 first = (__bf16)inv;
+                __bf16* parts = reinterpret_cast<__bf16*>(sVi[buf]);
+                parts[lane] = first;
+                parts[kStage + lane] = (__bf16)(inv - (float)first);
+            } else {
+                sVi[buf][lane] = inv;
+            }
+        }
     };
 
     auto barrier = [&]() {
@@ -300,7 +313,7 @@ __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams r
             if (t > -INFINITY) slack[rb] = kSlack;
             m[rb] += by;
             z[rb] *= corr;
-            if constexpr (STATS) z_plain[rb] *= corr;
+            if constexpr (ZM) { zr[rb][0] *= corr; zr[rb][1] *= corr; }
             s[rb] -= by;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) o[rb][dt] *= corr;
@@ -312,27 +325,27 @@ __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams r
         f32x16_t sn[RB];
         if constexpr (!LAST) products(sn);
         bf16x8_t pf[RB][2];
-        // Codes: a weight takes V's scale before it is rounded to bf16, and the sum takes the weight as it was rounded: where one key
-        // has nearly all of a row, as often, its rounding then cancels.  (Plain rows: such a key's weight is near 1, which bf16
-        // has.)  2-norm of the outputs' error in an int8 window, in that of their own rounding to bf16: 1.04 to 1.25 over four
-        // random inputs, with the plain sum up to 1.53.
+        // Codes: a weight takes V's scale before it is rounded to bf16, and what the outputs are divided by is the sum of the weights
+        // as they were rounded, over the scales: where one key has nearly all of a row, as often, its rounding then cancels.  (Plain
+        // rows: such a key's weight is near 1, which bf16 has.)  2-norm of the outputs' error in an int8 window, in that of their
+        // own rounding to bf16: 1.04 to 1.25 over four random inputs, with the plain sum up to 1.53.  The sum is another product
+        // of the weights, with 1 / scale as the sum of two bf16 numbers in the place of V (FP8, 2048 tokens over 32768: 1191 -> 1159 us),
+        // but for calls over 64-wide heads without statistics, where its 32 registers do not fit (770 -> 804): there the vector unit adds.
         float f[16] = {}, inv[16] = {};
-        if constexpr (Q8) {
-            scales_of(&sVs[0][0], j, f);
-            scales_of(&sVi[0][0], j, inv);
-        }
+        if constexpr (Q8) scales_of(&sVs[0][0], j, f);
+        if constexpr (Q8 && !ZM) scales_of(&sVi[0][0], j, inv);
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-            float zs[2] = {0.f, 0.f}, zp[2] = {0.f, 0.f};
+            float zs[2] = {0.f, 0.f};
             u32x4_t w4[2];
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
                 float p[2] = {exp2_fast(s[rb][i]), exp2_fast(s[rb][i + 1])}, to_p[2] = {inv[i], inv[i + 1]};
-                if constexpr (!Q8) {
+                if constexpr (!Q8 || STATS) {
                     zs[0] += p[0];
                     zs[1] += p[1];
-                } else {
-                    if constexpr (STATS) { zp[0] += p[0]; zp[1] += p[1]; }
+                }
+                if constexpr (Q8) {
                     p[0] *= f[i];
                     p[1] *= f[i + 1];
                     if constexpr (MASKED) {            // any scale stands behind keys that are not seen
@@ -347,7 +360,7 @@ __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams r
                 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
                 const uint32_t w = __builtin_bit_cast(uint32_t, bf16x2_t{(__bf16)p[0], (__bf16)p[1]});
                 w4[i >> 3][(i >> 1) & 3] = w;
-                if constexpr (Q8) {
+                if constexpr (Q8 && !ZM) {
                     zs[0] = fmaf(bf16_lo(w), to_p[0], zs[0]);
                     zs[1] = fmaf(bf16_hi(w), to_p[1], zs[1]);
                 }
@@ -355,7 +368,6 @@ __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams r
             pf[rb][0] = __builtin_bit_cast(bf16x8_t, w4[0]);
             pf[rb][1] = __builtin_bit_cast(bf16x8_t, w4[1]);
             z[rb] += zs[0] + zs[1];
-            if constexpr (STATS) z_plain[rb] += zp[0] + zp[1];
             asm volatile("" : "+v"(z[rb]));    // here, beside the products, not behind the step
         }
         if constexpr (!LAST) load_k(j + 2);
@@ -372,6 +384,17 @@ __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams r
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb) o[rb][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[rb][sp], o[rb][dt], 0, 0, 0);
             }
+        if constexpr (ZM) {
+            // rows of the first operand: the first parts of 1 / scale (even ones) and the second parts, in the order of the keys of pf
+            const uint16_t* at = reinterpret_cast<const uint16_t*>(sVi[(j >> 1) & (kRing - 1)]) + (lane & 1) * kStage + (j & 1) * 32 + 4 * half;
+#pragma unroll
+            for (int sp = 0; sp < 2; ++sp) {
+                const uint2 x = *reinterpret_cast<const uint2*>(at + 16 * sp), y = *reinterpret_cast<const uint2*>(at + 16 * sp + 8);
+                const bf16x8_t parts = __builtin_bit_cast(bf16x8_t, make_uint4(x.x, x.y, y.x, y.y));
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) zr[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(parts, pf[rb][sp], zr[rb], 0, 0, 0);
+            }
+        }
         if constexpr (LAST) return false;
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) asm volatile("" : "+v"(sn[rb]));       // out of the accumulation registers once, not for each use
@@ -453,9 +476,9 @@ __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams r
     for (int rb = 0; rb < RB; ++rb) {
         const int first = r0 + 32 * (RB * wave + rb), r = first + (lane & 31);
         const float top_m = max_across_halves(peak[rb]), to_top = top_m > kNoMax ? exp2_fast(m[rb] - top_m) : 1.f;     // relative to the largest logit from here on
-        const float zt = (z[rb] + __shfl_xor(z[rb], 32, kWave)) * to_top;
-        float zs = zt;
-        if constexpr (STATS) zs = (z_plain[rb] + __shfl_xor(z_plain[rb], 32, kWave)) * to_top;
+        const float zs = (z[rb] + __shfl_xor(z[rb], 32, kWave)) * to_top;       // the plain sum, if it was kept
+        float zt = zs;                                                          // what the outputs are divided by
+        if constexpr (ZM) zt = (zr[rb][0] + zr[rb][1]) * to_top;
         const float factor = a.n_units > 1 ? to_top : zt == 0.f ? 0.f : to_top / zt;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)

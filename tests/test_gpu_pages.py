@@ -284,6 +284,29 @@ def test_infinities_of_v_that_are_seen(dtype, cn):
     U.within(got[good], ref[0][good], U.bounds(ref, dtype, d, n)[0][good], "elsewhere")
 
 
+@pytest.mark.parametrize("fmt", ["fp8", "int8"])
+@pytest.mark.parametrize("d,g,cn", [(64, 1, 100), (64, 2, 300), (128, 2, 60), (128, 1, 300)])
+@pytest.mark.parametrize("stats", [False, True])
+def test_rows_of_the_chunk_without_a_number_reach_later_rows_only(fmt, d, g, cn, stats):
+    """NaN rows of quantised V and K in the chunk: earlier rows are as without them, rows from them on are NaN."""
+    n, at_v, at_k = cn + 200, cn // 3, cn // 2
+
+    def edit(k, v):
+        v[0, 0, 0, 200 + at_v, 5] = float("nan")
+        k[0, 0, 0, 200 + at_k, 1] = float("inf")
+    c = U.Case(1, g, 1, d, [(n, cn)], fmt=fmt, k_edit=edit)
+    c.fill()
+    out, M, Z = c.attn(stats=stats)
+    torch.cuda.synchronize()
+    ref = U.attention(c.q[0, 0, :, :cn], U.held(c.k[0, 0], fmt), U.held(c.v[0, 0], fmt), c.scale[0].item(), n, cn)
+    bo, bm, bz = U.bounds(ref, "bf16", d, n)
+    U.within(out[0, 0, :, :at_v], ref[0][:, :at_v], bo[:, :at_v], "rows before")
+    assert bool(torch.isnan(out[0, 0, :, at_v:cn]).all())
+    if stats:
+        U.within(M[0, 0, :, :at_k], ref[1][:, :at_k], bm[:, :at_k], "max")
+        U.within(Z[0, 0, :, :at_k], ref[2][:, :at_k], (bz * ref[2])[:, :at_k], "sum")
+
+
 def test_requests_that_share_pages_and_calls_without_lengths():
     """Two requests continue one prompt: its pages stand in both rows of the table; the lengths are the chunk's bounds."""
     import paper_2410_23317_amd as V
