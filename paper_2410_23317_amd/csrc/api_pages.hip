@@ -234,7 +234,9 @@ vlc_status vlc_pages_attn(vlc_pages* pages, const vlc_chunk* chunk, int32_t laye
         if (vlc_status st = check_rows(who, "k_new", k_new, s.dtype, false, nl, chunk->B, s.Hkv, chunk->max_new)) return st;
         if (vlc_status st = check_rows(who, "v_new", v_new, s.dtype, false, nl, chunk->B, s.Hkv, chunk->max_new)) return st;
     }
+    if (((uintptr_t)sm_scale & 3) != 0) return fail(VLC_ERR_INVALID_ARG, "%s: sm_scale must be 4-byte aligned", who);
     if (stats) {
+        if ((((uintptr_t)stats->row_max | (uintptr_t)stats->row_sum) & 3) != 0) return fail(VLC_ERR_INVALID_ARG, "%s: row_max and row_sum must be 4-byte aligned", who);
         if (!stats->row_max || !stats->row_sum) return fail(VLC_ERR_INVALID_ARG, "%s: stats without row_max or row_sum", who);
         const int64_t stride[3] = {stats->layer, stats->request, stats->head}, extent[3] = {nl, chunk->B, s.Hq};
         for (int x = 0; x < 3; ++x)

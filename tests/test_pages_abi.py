@@ -137,6 +137,16 @@ def test_calls_are_refused_before_any_launch(V):
     lib.vlc_pages_destroy(h)
 
 
+def test_floats_off_their_alignment_are_refused(V):
+    s, n, h, st = create(V)
+    R, K = C.byref(rows_of(V)), C.byref(chunk_of(V, max_len=16, max_new=1))
+    for scale, m, z in ((4098, 4096, 4096), (4096, 4097, 4096), (4096, 4096, 4102)):
+        stats = V.vlc_row_stats(m, z, 1000, 100, 5)
+        assert V.lib.vlc_pages_attn(h, K, 0, 2, R, None, None, scale, R, C.byref(stats), None, 0, None) == V.VLC_ERR_INVALID_ARG
+        assert "aligned" in V.vlc_last_error_string()
+    V.lib.vlc_pages_destroy(h)
+
+
 def test_formats_of_the_comparison_are_the_definitions():
     rng = np.random.default_rng(3)
     x = rng.standard_normal((200, 64)).astype(np.float32) * np.exp(rng.uniform(-20, 20, (200, 1))).astype(np.float32)
