@@ -162,7 +162,10 @@ class PagedPrompt:
         return self.chunk
 
     def _used(self, *tensors) -> None:
-        """These own tensors are read on the current stream, which may be another than the one they were made on."""
+        """These own tensors are read on the current stream, which may be another than the one they were made on.  Not while it is
+        captured: the next chunk replaces them, and a graph would go on using the old ones (vlc_pages_attn takes a caller's own)."""
+        if torch.cuda.is_current_stream_capturing():
+            raise ValueError("PagedPrompt replaces its lengths and workspace from chunk to chunk and is not captured")
         stream = torch.cuda.current_stream(self.device)
         for t in tensors:
             if t is not None:
@@ -172,10 +175,11 @@ class PagedPrompt:
         """The chunk's rows of layers [layer_begin, layer_end) into the pages, and their attention."""
         if self.chunk is None:
             raise ValueError("begin_chunk() comes first")
+        self._used(self.chunk.tensors[1])
         need = V.vlc_pages_attn_workspace_bytes(self.pages, self.chunk, layer_end - layer_begin)
         if need and (self.workspace is None or self.workspace.numel() < need):
             self.workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
-        self._used(self.workspace, self.chunk.tensors[1])
+        self._used(self.workspace)
         V.vlc_pages_attn(self.pages, self.chunk, layer_begin, layer_end, q, k_new, v_new, sm_scale, out, row_max, row_sum, self.workspace)
 
     def read(self, k_out, v_out) -> None:

@@ -307,6 +307,24 @@ def test_rows_of_the_chunk_without_a_number_reach_later_rows_only(fmt, d, g, cn,
         U.within(Z[0, 0, :, :at_k], ref[2][:, :at_k], (bz * ref[2])[:, :at_k], "sum")
 
 
+def test_a_prompt_in_chunks_is_not_captured():
+    from paper_2410_23317_amd import pipeline
+    p = pipeline.PagedPrompt(1, 2, 1, 64, torch.bfloat16, 1, 100, page_slots=16)
+    q, kv, out = (torch.zeros((1, 1, h, 4, 64), dtype=torch.bfloat16, device="cuda") for h in (2, 1, 2))
+    p.begin_chunk([4])
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out.zero_()
+        with pytest.raises(ValueError):
+            p.extend(0, 1, q, kv, kv, None, out)
+        with pytest.raises(ValueError):
+            p.read(kv, kv)
+    g.replay()
+    p.extend(0, 1, q, kv, kv, None, out)
+    p.status()
+
+
 def test_requests_that_share_pages_and_calls_without_lengths():
     """Two requests continue one prompt: its pages stand in both rows of the table; the lengths are the chunk's bounds."""
     import paper_2410_23317_amd as V
