@@ -13,7 +13,7 @@
 // block of 128-wide heads, and two blocks of four waves of 64 rows fit a compute unit with 64-wide ones.  2048 tokens of 32
 // heads over 32768 keys, us (TFLOP/s): d = 128 one wave per SIMD with 64 rows 1028, two with 32 rows 993 (1073); d = 64 one 811,
 // two 588 (905).  A large bf16 matrix product reaches 1256 TFLOP/s here; neither more lookahead, other wave priorities nor
-// none of the lookahead moves the 993 by 1 %.  FP8 pages 1159, int8 1192 (d = 64: 781): the codes' expansion, two scales, and
+// none of the lookahead moves the 993 by 1 %.  FP8 pages 1144, int8 about 1190 (d = 64: 781): the codes' expansion, two scales, and
 // the sum over rounded weights (see step; 5 % of the time with d = 128, 13 % with 64).
 //
 // A row's weights are relative to m, which starts as the maximum of its first 32 keys and is raised only when a logit exceeds
@@ -25,7 +25,7 @@
 // three stages ahead; codes are fetched into registers, expanded to bf16 (exactly) on their way into LDS, and their scales
 // multiply the logits and the probabilities.  Probabilities are rounded to bf16 for the product with V, a half step of 2^-8
 // each; the sums are fp32, of the probabilities themselves for plain rows and of the rounded ones for codes.  16-byte pieces of a row lie at swizzled places, so that neither the
-// reads of K (16 rows, one piece) nor the transposing reads of V (four rows, 64 bytes) meet on a bank (counted: no conflicts).
+// reads of K (16 rows, one piece) nor the transposing reads of V (four rows, 64 bytes) meet on a bank (counted: no conflicts; the writes of expanded codes have some, 3 % of the cycles).
 #include "pages_rows.h"
 #include "score_tiles.h"
 
@@ -67,13 +67,14 @@ template <int D, int FMT, int RB, int W, bool STATS>
 __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams ra) {
     constexpr int kWaves = W, kThreads = W * 64, kRows = 32 * RB * W;
     constexpr bool Q8 = PageRow<FMT>::kQuantised;
-    constexpr bool ZM = Q8 && (D == 128 || STATS);             // who adds the rounded weights up: the matrix unit, or the vector unit (see step)
     constexpr int KS = D / 16, DT = D / 32, PPR = D / 8;       // k-steps of K Q^T, 32-wide tiles of d, pieces per row
     constexpr int ROWB = D * PageRow<FMT>::kElemBytes;         // bytes of a row in a page
     constexpr int LOADS = 2 * kStage * PPR / kThreads;         // 16-byte pieces of K and V per thread and stage (plain rows)
+    constexpr bool ZM = Q8 && (D == 128 || STATS);             // who adds the rounded weights up: the matrix unit, or the vector unit (see step)
+    constexpr int kSecond = kStage + 8;                        // where the second parts start: on other banks than the first
     __shared__ __align__(1024) uint4 sK[kRing][kStage * PPR];
     __shared__ __align__(1024) uint4 sV[kRing][kStage * PPR];
-    __shared__ __align__(16) float sKs[Q8 ? kRing : 1][kStage], sVs[Q8 ? kRing : 1][kStage], sVi[Q8 ? kRing : 1][kStage];      // scales; 1 / V's: fp32, or all first and all second parts
+    __shared__ __align__(16) float sKs[Q8 ? kRing : 1][kStage], sVs[Q8 ? kRing : 1][kStage], sVi[Q8 ? kRing : 1][ZM ? kStage + 4 : kStage];      // scales; 1 / V's: fp32, or all first and all second parts
     __shared__ int sBad[2];            // first and last stage in which numbers of V were replaced by 0
     const PagesAttnParams& a = ra.a;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
@@ -217,7 +218,7 @@ __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams r
                 const __bf16 first = (__bf16)inv;
                 __bf16* parts = reinterpret_cast<__bf16*>(sVi[buf]);
                 parts[lane] = first;
-                parts[kStage + lane] = (__bf16)(inv - (float)first);
+                parts[kSecond + lane] = (__bf16)(inv - (float)first);
             } else {
                 sVi[buf][lane] = inv;
             }
@@ -329,7 +330,7 @@ __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams r
         // as they were rounded, over the scales: where one key has nearly all of a row, as often, its rounding then cancels.  (Plain
         // rows: such a key's weight is near 1, which bf16 has.)  2-norm of the outputs' error in an int8 window, in that of their
         // own rounding to bf16: 1.04 to 1.25 over four random inputs, with the plain sum up to 1.53.  The sum is another product
-        // of the weights, with 1 / scale as the sum of two bf16 numbers in the place of V (FP8, 2048 tokens over 32768: 1191 -> 1159 us),
+        // of the weights, with 1 / scale as the sum of two bf16 numbers in the place of V (FP8, 2048 tokens over 32768: 1191 -> 1144 us),
         // but for calls over 64-wide heads without statistics, where its 32 registers do not fit (770 -> 804): there the vector unit adds.
         float f[16] = {}, inv[16] = {};
         if constexpr (Q8) scales_of(&sVs[0][0], j, f);
@@ -386,7 +387,7 @@ __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams r
             }
         if constexpr (ZM) {
             // rows of the first operand: the first parts of 1 / scale (even ones) and the second parts, in the order of the keys of pf
-            const uint16_t* at = reinterpret_cast<const uint16_t*>(sVi[(j >> 1) & (kRing - 1)]) + (lane & 1) * kStage + (j & 1) * 32 + 4 * half;
+            const uint16_t* at = reinterpret_cast<const uint16_t*>(sVi[(j >> 1) & (kRing - 1)]) + (lane & 1) * kSecond + (j & 1) * 32 + 4 * half;
 #pragma unroll
             for (int sp = 0; sp < 2; ++sp) {
                 const uint2 x = *reinterpret_cast<const uint2*>(at + 16 * sp), y = *reinterpret_cast<const uint2*>(at + 16 * sp + 8);
