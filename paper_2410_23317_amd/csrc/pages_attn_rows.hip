@@ -24,8 +24,9 @@
 // Keys come in stages of 64 through a ring of four LDS buffers: plain rows go from memory to LDS without registers, requested
 // three stages ahead; codes are fetched into registers, expanded to bf16 (exactly) on their way into LDS, and their scales
 // multiply the logits and the probabilities.  Probabilities are rounded to bf16 for the product with V, a half step of 2^-8
-// each; the sums are fp32, of the probabilities themselves for plain rows and of the rounded ones for codes.  16-byte pieces of a row lie at swizzled places, so that neither the
-// reads of K (16 rows, one piece) nor the transposing reads of V (four rows, 64 bytes) meet on a bank (counted: no conflicts; the writes of expanded codes have some, 3 % of the cycles).
+// each; the sums are fp32, of the probabilities themselves for plain rows and of the rounded ones for codes.  16-byte pieces of a
+// row lie at swizzled places, so that neither the reads of K (16 rows, one piece) nor the transposing reads of V (four rows, 64
+// bytes) meet on a bank (counted: no conflicts; the writes of expanded codes have some, 3 % of the cycles).
 #include "pages_rows.h"
 #include "score_tiles.h"
 
@@ -74,7 +75,8 @@ __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams r
     constexpr int kSecond = kStage + 8;                        // where the second parts start: on other banks than the first
     __shared__ __align__(1024) uint4 sK[kRing][kStage * PPR];
     __shared__ __align__(1024) uint4 sV[kRing][kStage * PPR];
-    __shared__ __align__(16) float sKs[Q8 ? kRing : 1][kStage], sVs[Q8 ? kRing : 1][kStage], sVi[Q8 ? kRing : 1][ZM ? kStage + 4 : kStage];      // scales; 1 / V's: fp32, or all first and all second parts
+    __shared__ __align__(16) float sKs[Q8 ? kRing : 1][kStage], sVs[Q8 ? kRing : 1][kStage], sVi[Q8 ? kRing : 1][ZM ? kStage + 4 : kStage];
+    // (scales; sVi: 1 / V's as fp32, or all first and all second parts)
     __shared__ int sBad[2];            // first and last stage in which numbers of V were replaced by 0
     const PagesAttnParams& a = ra.a;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
