@@ -448,7 +448,8 @@ vlc_status vlc_pages_status(vlc_pages* pages, vlc_stream stream);
  *            for every request.  A request may have no new tokens (c_b = 0), or be empty.
  *   max_new  rows per request in the chunk's tensors; max_len bounds n_b and sizes the launch (a captured graph whose
  *            lens grow from replay to replay takes the largest):  1 <= max_new <= max_len <= max_pages * page_slots, max_len <= 2^25
- * Both arrays are read when a call's kernels run.  A request whose lengths break these bounds is skipped, an entry of the
+ * Both arrays are read when a call's kernels run.  A request whose lengths break these bounds is skipped (vlc_pages_read looks
+ * at n_b alone, 0 <= n_b <= max_len), an entry of the
  * table outside [0, n_pages) is taken as page 0 for reading (that request's results are then meaningless) and not written
  * to; either sets the sticky status to VLC_ERR_INVALID_ARG.  Requests may share pages that no call writes to; two rows
  * written to one slot by one call leave it undefined. */
@@ -479,7 +480,8 @@ vlc_status vlc_pages_write(vlc_pages* pages, const vlc_chunk* chunk, int32_t lay
 /*
  * vlc_pages_read -- positions [first, min(n_b, first + count)) of every request, as rows 0.. of k_out and v_out
  * [layers in range, B, Hkv, count, d], storage dtype: the row itself, or fp32(code * scale) rounded to nearest even.  Rows
- * beyond a request's are left as they are.  first >= 0, 1 <= count; chunk->max_new and c_b play no part.
+ * beyond a request's are left as they are.  first >= 0, 1 <= count; c_b plays no part, whatever it holds, and of chunk->max_new only
+ * that it lies in its own bounds.
  */
 vlc_status vlc_pages_read(vlc_pages* pages, const vlc_chunk* chunk, int32_t layer_begin, int32_t layer_end,
                           int32_t first, int32_t count, const vlc_rows* k_out, const vlc_rows* v_out, vlc_stream stream);

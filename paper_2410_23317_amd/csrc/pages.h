@@ -55,11 +55,21 @@ inline PagesParams pages_params(const PagesCall& c) {
     return p;
 }
 
-// Tokens of request b with the chunk (n) and in it (c); a request whose pair breaks the call's bounds counts as empty.
+// Tokens of request b with the chunk (n) and in it (c); a request whose pair breaks the call's bounds counts as empty.  Reading takes
+// no chunk: held_len looks at n alone.
 struct ChunkLen {
     int n, c;
     bool ok;
 };
+__device__ __forceinline__ ChunkLen held_len(const PagesParams& p, int b) {
+    ChunkLen r{p.max_len, 0, true};
+    if (p.lens) {
+        r.n = p.lens[2 * b];
+        r.ok = r.n >= 0 && r.n <= p.max_len;
+        if (!r.ok) r.n = 0;
+    }
+    return r;
+}
 __device__ __forceinline__ ChunkLen chunk_len(const PagesParams& p, int b) {
     ChunkLen r{p.max_len, p.max_new, true};
     if (p.lens) {

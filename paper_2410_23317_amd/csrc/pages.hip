@@ -62,7 +62,7 @@ __global__ __launch_bounds__(256) void pages_read_kernel(MoveArgs a) {
     typedef typename R::T T;
     constexpr int LPR = D * (int)sizeof(T) / 16;
     const int lb = blockIdx.y, l = lb / a.p.B, b = lb % a.p.B;
-    const ChunkLen len = chunk_len(a.p, b);
+    const ChunkLen len = held_len(a.p, b);
     const int sub = threadIdx.x % LPR;
     if (!len.ok && l == 0 && blockIdx.x == 0 && threadIdx.x == 0) report_lens(a.p, b);
     const int x = blockIdx.x * (256 / LPR) + threadIdx.x / LPR;

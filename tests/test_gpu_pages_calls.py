@@ -1,0 +1,38 @@
+"""Calls on the paged prompt cache that its documentation allows, at the borders of what the other tests make, against the
+definitions in 64 bits (pages_util)."""
+import pytest
+import torch
+
+import pages_util as U
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("fmt,dtype", U.FORMATS)
+def test_a_read_takes_no_chunk(fmt, dtype):
+    """The lengths of the last chunk, of a padded batch, and no sensible c_b at all, read with a bound of one new row: n_b
+    alone says what is there.  An n_b out of bounds is still reported, and its request left alone."""
+    import paper_2410_23317_amd as V
+    L, H, d, lens = 2, 2, 64, [(50, 7), (33, 33), (20, 1), (41, 0)]
+    c = U.Case(L, 2 * H, H, d, lens, fmt=fmt, dtype=dtype)
+    c.fill()
+    chunk = V.make_chunk(c.table, 1, c.max_len, c.lens_t)
+    for cb in (None, -5, 1 << 30):
+        if cb is not None:
+            c.lens_t[:, 1] = cb
+        outs = [torch.full_like(c.k, 5.0) for _ in range(2)]
+        V.vlc_pages_read(c.pages, chunk, 0, L, 0, *outs)
+        V.vlc_pages_status(c.pages)
+        for got, src in zip(outs, (c.k, c.v)):
+            for b, (n, _) in enumerate(lens):
+                assert torch.equal(got[:, b, :, :n].cpu(), U.held(src[:, b, :, :n], fmt).float().to(U.storage(dtype))), (cb, b)
+                assert bool((got[:, b, :, n:] == 5.0).all())
+    for n in (-1, c.max_len + 1):
+        c.lens_t[1, 0] = n
+        ko, vo = torch.full_like(c.k, 5.0), torch.full_like(c.v, 5.0)
+        V.vlc_pages_read(c.pages, chunk, 0, L, 0, ko, vo)
+        with pytest.raises(V.VlcError, match="request 1: lengths"):
+            V.vlc_pages_status(c.pages)
+        assert bool((ko[:, 1] == 5.0).all()) and bool((vo[:, 1] == 5.0).all())
+        assert torch.equal(ko[:, 0].cpu(), U.held(c.k[:, 0], fmt).float().to(U.storage(dtype)))
+        V.vlc_pages_clear(c.pages)
