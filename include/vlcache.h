@@ -407,8 +407,11 @@ vlc_status vlc_decode_attn_steps(vlc_cache* cache, int32_t layer_begin, int32_t 
  *                    fp32(x / scale), ties to even
  * The scale of a row of zeros is 1, that of a row with an infinite or NaN entry is NaN (it reads back as NaN).
  *
- * Supported: d in {64, 128}; Hq % Hkv == 0 with g <= 8; L <= 1024; page_slots one of 16, 32, 64, 128, 256;
- * n_pages * page_slots <= 2^30. */
+ * Supported: d in {64, 128}; Hq % Hkv == 0 with g <= 8; Hkv <= 65535; L <= 1024; page_slots one of 16, 32, 64, 128, 256;
+ * n_pages * page_slots <= 2^30; L * n_pages * page_slots * Hkv * d <= 4e12.
+ * A call, whose layers are those of its range: B * layers * Hkv <= 65535 and B * layers * Hkv * (max_len / 1024 + 1) <= 2^23;
+ * vlc_pages_write max_new * Hkv <= 2^26; vlc_pages_read the same of count, or of max_len - first if that is less;
+ * vlc_pages_attn max_new * Hq <= 2^26 and B * layers * Hq * max_new <= 2^30.  VLC_ERR_SHAPE otherwise. */
 typedef enum { VLC_PAGES_PLAIN = 0, VLC_PAGES_FP8 = 1, VLC_PAGES_INT8 = 2 } vlc_pages_format;
 typedef struct {
     int32_t L, Hq, Hkv, d;
@@ -472,7 +475,6 @@ typedef struct {
 /*
  * vlc_pages_write -- the c_b new rows of K and V of every request into its pages, layers [layer_begin, layer_end),
  * quantised if the pages are.  k_new, v_new: [layers in range, B, Hkv, max_new, d], storage dtype; rows >= c_b are not read.
- * B * layers in range * Hkv <= 65535 here and in the two calls below.
  */
 vlc_status vlc_pages_write(vlc_pages* pages, const vlc_chunk* chunk, int32_t layer_begin, int32_t layer_end,
                            const vlc_rows* k_new, const vlc_rows* v_new, vlc_stream stream);

@@ -64,10 +64,23 @@ vlc_status check_call(const char* who, const vlc_pages* pages, const vlc_chunk* 
     if (c->max_new < 1 || c->max_new > c->max_len || c->max_len > (int64_t)c->max_pages * s.page_slots || c->max_len > 1 << 25)
         return fail(VLC_ERR_SHAPE, "%s: 1 <= max_new = %d <= max_len = %d <= max_pages * page_slots = %lld (and 2^25) does not hold", who,
                     c->max_new, c->max_len, (long long)c->max_pages * s.page_slots);
-    // grids of fewer than 2^24 blocks
-    if ((int64_t)c->B * n_layers * s.Hkv * (c->max_len / 1024 + 1) > 1 << 23 || (int64_t)c->B * n_layers * s.Hq * c->max_new > (int64_t)1 << 30)
-        return fail(VLC_ERR_SHAPE, "%s: B * layers * Hkv * max_len exceeds 2^33, or B * layers * Hq * max_new 2^30", who);
+    if ((int64_t)c->B * n_layers * s.Hkv * (c->max_len / 1024 + 1) > 1 << 23)
+        return fail(VLC_ERR_SHAPE, "%s: B * layers * Hkv * (max_len / 1024 + 1) exceeds 2^23", who);
+    return VLC_OK;
+}
+
+// What an attention call takes of query rows: with it and the limit above, its grids have fewer than 2^24 blocks.
+vlc_status check_queries(const char* who, const vlc_pages* pages, const vlc_chunk* c, int64_t n_layers) {
+    const vlc_pages_shape& s = pages->shape;
+    if ((int64_t)c->B * n_layers * s.Hq * c->max_new > (int64_t)1 << 30) return fail(VLC_ERR_SHAPE, "%s: B * layers * Hq * max_new exceeds 2^30", who);
     if ((int64_t)c->max_new * s.Hq > 1 << 26) return fail(VLC_ERR_SHAPE, "%s: max_new * Hq = %lld exceeds 2^26", who, (long long)c->max_new * s.Hq);
+    return VLC_OK;
+}
+
+// Rows that a launch of the writer or the reader moves per (layer, request): at most 2^23 blocks along x.
+vlc_status check_moved(const char* who, const vlc_pages* pages, const char* name, int rows) {
+    const int64_t n = (int64_t)rows * pages->shape.Hkv;
+    if (n > 1 << 26) return fail(VLC_ERR_SHAPE, "%s: %s * Hkv = %lld exceeds 2^26", who, name, (long long)n);
     return VLC_OK;
 }
 
@@ -177,6 +190,7 @@ vlc_status vlc_pages_write(vlc_pages* pages, const vlc_chunk* chunk, int32_t lay
     if (vlc_status st = check_layers(who, pages, layer_begin, layer_end)) return st;
     const int64_t nl = layer_end - layer_begin;
     if (vlc_status st = check_call(who, pages, chunk, nl)) return st;
+    if (vlc_status st = check_moved(who, pages, "max_new", chunk->max_new)) return st;
     const vlc_pages_shape& s = pages->shape;
     if (vlc_status st = check_rows(who, "k_new", k_new, s.dtype, false, nl, chunk->B, s.Hkv, chunk->max_new)) return st;
     if (vlc_status st = check_rows(who, "v_new", v_new, s.dtype, false, nl, chunk->B, s.Hkv, chunk->max_new)) return st;
@@ -198,7 +212,7 @@ vlc_status vlc_pages_read(vlc_pages* pages, const vlc_chunk* chunk, int32_t laye
     if (vlc_status st = check_rows(who, "v_out", v_out, s.dtype, true, nl, chunk->B, s.Hkv, count)) return st;
     if (first >= chunk->max_len) return VLC_OK;               // no request holds such a position
     if (count > chunk->max_len - first) count = chunk->max_len - first;
-    if ((int64_t)count * s.Hkv > 1 << 26) return fail(VLC_ERR_SHAPE, "%s: count * Hkv = %lld exceeds 2^26", who, (long long)count * s.Hkv);
+    if (vlc_status st = check_moved(who, pages, "count", count)) return st;
     if (vlc_status st = check_cleared(who, pages)) return st;
     const hipError_t e = vlc::launch_pages_read(pages_call(pages, chunk, layer_begin, layer_end, stream), first, count, *k_out, *v_out);
     if (e != hipSuccess) return hip_fail(e, who);
@@ -211,6 +225,7 @@ vlc_status vlc_pages_attn_workspace_bytes(const vlc_pages* pages, const vlc_chun
     *bytes_out = 0;
     if (vlc_status st = check_layers(who, pages, 0, n_layers)) return st;
     if (vlc_status st = check_call(who, pages, chunk, n_layers)) return st;
+    if (vlc_status st = check_queries(who, pages, chunk, n_layers)) return st;
     const vlc::PagesCall c = pages_call(pages, chunk, 0, n_layers, nullptr);
     *bytes_out = vlc::pages_few_supported(c) ? vlc::pages_few_workspace_bytes(c)
                  : c.s.dtype == VLC_F32        ? vlc::pages_rows_f32_workspace_bytes(c)
@@ -225,6 +240,7 @@ vlc_status vlc_pages_attn(vlc_pages* pages, const vlc_chunk* chunk, int32_t laye
     if (vlc_status st = check_layers(who, pages, layer_begin, layer_end)) return st;
     const int64_t nl = layer_end - layer_begin;
     if (vlc_status st = check_call(who, pages, chunk, nl)) return st;
+    if (vlc_status st = check_queries(who, pages, chunk, nl)) return st;
     const vlc_pages_shape& s = pages->shape;
     if (vlc_status st = check_rows(who, "q", q, s.dtype, false, nl, chunk->B, s.Hq, chunk->max_new)) return st;
     if (vlc_status st = check_rows(who, "out", out, s.dtype, true, nl, chunk->B, s.Hq, chunk->max_new)) return st;
