@@ -152,6 +152,8 @@ struct FewTile {                                // bf16 operands
             }
         }
     }
+    // A logit is rounded before the maximum is taken off: |s| 2^-24 of its weight, less than the output's rounding up to |s| = 2^15.
+    // (Taking it off in one fma, as fp32 storage does, makes Q wait for the scale's sign: one token 9.95 -> 10.25 us.)
     template <bool MASKED>
     __device__ __forceinline__ void logits(const Columns<NT>& col, float scale2, int t0, int lane) {
 #pragma unroll
@@ -199,7 +201,7 @@ struct FewTile {                                // bf16 operands
         return bad;
     }
     template <bool MASKED>
-    __device__ __forceinline__ void outputs(const Columns<NT>& col, int t0, int lane) {
+    __device__ __forceinline__ void outputs(const Columns<NT>& col, float, int t0, int lane) {
         bf16x8_t pb[NT], pl[NT];                                // weights as two bf16 numbers: what the first leaves over in the second
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -306,8 +308,18 @@ struct FewTile<D, kPageF32, NT> {               // fp32 operands
             }
         }
     }
+    // x holds the products Q K^T: the maximum is taken off their logits with one rounding, of the difference (fp32 outputs show
+    // the rounding of a large logit).  Q takes the sign of a scale that is not positive, or is 0 for a scale of 0, so that the
+    // largest product is the largest logit.
+    __device__ __forceinline__ void sign_q(float scale) {
+        const float sign = scale < 0.f ? -1.f : scale == 0.f ? 0.f : 1.f;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int s = 0; s < KP; ++s) qf[nt][s] *= sign;
+    }
     template <bool MASKED>
-    __device__ __forceinline__ void logits(const Columns<NT>& col, float scale2, int t0, int lane) {
+    __device__ __forceinline__ void logits(const Columns<NT>& col, float, int t0, int lane) {
         f32x4_t s[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) s[nt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -321,7 +333,7 @@ struct FewTile<D, kPageF32, NT> {               // fp32 operands
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float v = s[nt][i] * scale2;
+                float v = s[nt][i];
                 if (MASKED) v = t0 + 4 * (lane >> 4) + i <= col.last[nt] ? v : -INFINITY;
                 x[nt][i] = v;
             }
@@ -344,14 +356,14 @@ struct FewTile<D, kPageF32, NT> {               // fp32 operands
         return bad;
     }
     template <bool MASKED>
-    __device__ __forceinline__ void outputs(const Columns<NT>&, int, int) {
+    __device__ __forceinline__ void outputs(const Columns<NT>&, float scale2, int, int) {
         float p[NT][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             float mt = x[nt][0];
 #pragma unroll
             for (int j = 1; j < 4; ++j) mt = fmaxf(mt, x[nt][j]);
-            const float m_new = fmaxf(m_run[nt], max_over_groups(mt));
+            const float m_new = fmaxf(m_run[nt], max_over_groups(mt) * scale2);
             if (__any(m_new > m_run[nt])) {
                 const float corr = exp2_fast(m_run[nt] - m_new);
                 l_run[nt] *= corr;
@@ -360,7 +372,7 @@ struct FewTile<D, kPageF32, NT> {               // fp32 operands
                 m_run[nt] = m_new;
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) { p[nt][j] = exp2_fast(x[nt][j] - m_run[nt]); l_run[nt] += p[nt][j]; }
+            for (int j = 0; j < 4; ++j) { p[nt][j] = exp2_fast(fmaf(x[nt][j], scale2, -m_run[nt])); l_run[nt] += p[nt][j]; }
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -462,7 +474,14 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : NT == 2 || D == 64 ? 2 : 1)
         col.last[nt] = first_new + i;
         tile.begin(nt, (const T*)a.q.at(l, b, h * g + c - i * g, i), lane);
     }
-    const float scale2 = attn_scale(a, l, D) * kLog2e;
+    float scale = attn_scale(a, l, D);
+    if constexpr (FMT == kPageF32) {
+        if (!(scale > 0.f)) {
+            tile.sign_q(scale);
+            scale = scale == 0.f ? 1.f : -scale;
+        }
+    }
+    const float scale2 = scale * kLog2e;
 
     bool not_finite = false;                                    // numbers of V were replaced by 0 in a tile
     // Positions behind the last one are read too (slots of the same page, or of page 0 in place of a page that is not there).
@@ -484,13 +503,13 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : NT == 2 || D == 64 ? 2 : 1)
         for (; t0 + STEP < end; t0 += STEP) {
             tile.template logits<false>(col, scale2, t0, lane);
             tile.request_k(r, t0 + STEP, lane);
-            tile.template outputs<false>(col, t0, lane);
+            tile.template outputs<false>(col, scale2, t0, lane);
             tile.request_v(r, t0 + STEP, lane);
         }
         if (fresh) tile.take_new(sNew, first_new, end, t0, lane);
         tile.template logits<true>(col, scale2, t0, lane);
         if (t0 + TK > first_new + 1) not_finite = tile.clean_v(col, t0, lane);
-        tile.template outputs<true>(col, t0, lane);
+        tile.template outputs<true>(col, scale2, t0, lane);
     }
 
     if (__any(not_finite)) {

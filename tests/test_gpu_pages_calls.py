@@ -36,3 +36,28 @@ def test_a_read_takes_no_chunk(fmt, dtype):
         assert bool((ko[:, 1] == 5.0).all()) and bool((vo[:, 1] == 5.0).all())
         assert torch.equal(ko[:, 0].cpu(), U.held(c.k[:, 0], fmt).float().to(U.storage(dtype)))
         V.vlc_pages_clear(c.pages)
+
+
+@pytest.mark.parametrize("Hq,cn", [(1, 1), (4, 1), (8, 2), (8, 4), (4, 30)])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_fp32_logits_that_are_large_and_close(Hq, cn, sign):
+    """Logits of 32000 to 32007, exact in fp32: weights take the difference from the maximum, of at most 7, not the rounding of
+    32007 log2 e (2^-9, which is 1e-3 of a weight).  Bound: the difference times log2 e carries log2 e's rounding (2^-24 of 10.1),
+    its own (2^-21 of less than 16), and the exponential's (2^-22); numerator and sum each: 2^-19 of the mean of |V|, and
+    8 sqrt(n) 2^-24 for the sums.  V is a function of the logit, so that errors of equal weights do not average out."""
+    n, d = cn + 200, 64
+
+    def edit(k, v):
+        at = torch.arange(n) * 5 % 8
+        k[..., :] = 0
+        k[..., 0] = sign * (32000 + at)
+        v[:] = torch.randn((8, d), generator=torch.Generator().manual_seed(cn))[at]
+    c = U.Case(1, Hq, 1, d, [(n, cn)], dtype="f32", k_edit=edit)
+    c.q.zero_()
+    c.q[..., 0] = 1
+    c.fill()
+    out, M, Z = c.attn(scale=torch.full((1,), sign, device="cuda"))
+    torch.cuda.synchronize()
+    ref = U.attention(c.q[0, 0], U.held(c.k[0, 0], "plain"), U.held(c.v[0, 0], "plain"), sign, n, cn)
+    U.within(out[0, 0], ref[0], (2.0 ** -18 + 16 * n ** 0.5 * 2.0 ** -24) * ref[3], "out")
+    U.within(M[0, 0], ref[1], 4 * 2.0 ** -24 * ref[1].abs(), "max")
