@@ -130,7 +130,9 @@ class PagedPrompt:
     """A batch of prompts that arrive in chunks, kept in pages until they are compressed.
 
     page_table [B, max_pages] names the pages of each request (int32, on the device); by default request b owns pages
-    b * max_pages .. of a pool with room for max_len tokens each.  The host keeps how many tokens each request holds."""
+    b * max_pages .. of a pool with room for max_len tokens each.  The host keeps how many tokens each request holds.
+    The constructor clears the pages on the stream that is current there; a call on another stream must wait for it.  Dropping the
+    object while such a stream still works on it is safe: its own tensors stay allocated until that work is done."""
 
     def __init__(self, L: int, Hq: int, Hkv: int, d: int, dtype, B: int, max_len: int, page_slots: int = 64, format="plain",
                  n_pages: Optional[int] = None, page_table: Optional[torch.Tensor] = None, device: str = "cuda"):
@@ -143,7 +145,7 @@ class PagedPrompt:
         self.table = page_table
         self.pages = V.vlc_pages_create(V.make_pages_shape(L, Hq, Hkv, d, page_slots, n_pages or B * max_pages, dtype, format), device)
         self.tokens = [0] * B
-        self.device = torch.device(device)
+        self.device = self.pages.arena.device
         self.workspace = None
         self.chunk = None
 
@@ -162,12 +164,13 @@ class PagedPrompt:
         return self.chunk
 
     def _used(self, *tensors) -> None:
-        """These own tensors are read on the current stream, which may be another than the one they were made on.  Not while it is
-        captured: the next chunk replaces them, and a graph would go on using the old ones (vlc_pages_attn takes a caller's own)."""
+        """The pages, the table and these own tensors are used on the current stream, which may be another than the one they were
+        made on.  Not while it is captured: the next chunk replaces lengths and workspace, and a graph would go on using the old
+        ones (vlc_pages_attn takes a caller's own)."""
         if torch.cuda.is_current_stream_capturing():
             raise ValueError("PagedPrompt replaces its lengths and workspace from chunk to chunk and is not captured")
         stream = torch.cuda.current_stream(self.device)
-        for t in tensors:
+        for t in (self.pages.arena, self.table, *tensors):
             if t is not None:
                 t.record_stream(stream)
 

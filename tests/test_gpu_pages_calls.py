@@ -61,3 +61,22 @@ def test_fp32_logits_that_are_large_and_close(Hq, cn, sign):
     ref = U.attention(c.q[0, 0], U.held(c.k[0, 0], "plain"), U.held(c.v[0, 0], "plain"), sign, n, cn)
     U.within(out[0, 0], ref[0], (2.0 ** -18 + 16 * n ** 0.5 * 2.0 ** -24) * ref[3], "out")
     U.within(M[0, 0], ref[1], 4 * 2.0 ** -24 * ref[1].abs(), "max")
+
+
+def test_a_prompt_dropped_while_a_stream_works_on_it_keeps_its_memory():
+    """A side stream is still busy when the prompt goes: its arena and table are not handed out again before that stream is done."""
+    from paper_2410_23317_amd import pipeline
+    p = pipeline.PagedPrompt(1, 2, 1, 64, torch.bfloat16, 1, 5000, page_slots=16)
+    q, kv, out = (torch.zeros((1, 1, h, 4, 64), dtype=torch.bfloat16, device="cuda") for h in (2, 1, 2))
+    p.begin_chunk([4])
+    torch.cuda.synchronize()
+    size, was = p.pages.arena.numel(), p.pages.arena.data_ptr()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(400_000_000)                           # some tenths of a second
+        p.extend(0, 1, q, kv, kv, None, out)
+    p = None
+    busy = not side.query()
+    later = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    assert busy and was not in [t.data_ptr() for t in later]
+    side.synchronize()

@@ -1,0 +1,60 @@
+"""pipeline.PagedPrompt without a GPU: what it tells the allocator and what it keeps of the requests' lengths, over stand-ins for
+its device tensors."""
+from types import SimpleNamespace
+
+import pytest
+import torch
+
+from test_pages_abi import V  # noqa: F401
+
+
+class DeviceTensor:
+    def __init__(self, n=1 << 20):
+        self.n, self.streams = n, []
+
+    def record_stream(self, s):
+        self.streams.append(s)
+
+    def numel(self):
+        return self.n
+
+    def transpose(self, *a):
+        return self
+
+
+@pytest.fixture
+def prompt(V, monkeypatch):
+    """A prompt of two requests with room for 100 tokens whose library calls do nothing but can be made to fail."""
+    from paper_2410_23317_amd import pipeline
+    p = object.__new__(pipeline.PagedPrompt)
+    p.max_len, p.tokens, p.chunk, p.workspace, p.device = 100, [0, 0], None, DeviceTensor(), torch.device("cpu")
+    p.table, p.pages = DeviceTensor(), SimpleNamespace(arena=DeviceTensor(), shape=SimpleNamespace(L=1))
+    p.calls, p.fail = [], False
+
+    def call(name):
+        def made(*a):
+            if p.fail:
+                raise ValueError(name)
+            p.calls.append(name)
+            return 0
+        return made
+    for name in ("vlc_pages_attn", "vlc_pages_read", "vlc_pages_attn_workspace_bytes"):
+        monkeypatch.setattr(pipeline.V, name, call(name))
+    monkeypatch.setattr(pipeline.V, "make_chunk", lambda table, max_new, max_len, lens: SimpleNamespace(
+        tensors=(table, DeviceTensor()), lens=lens.tolist(), max_new=max_new, max_len=max_len))
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: "side")
+    return p
+
+
+def test_everything_a_call_works_on_is_recorded_on_its_stream(prompt):
+    """What is dropped while another stream than the one it was made on works with it must not be handed out again before that."""
+    prompt.begin_chunk([3, 5])
+    lens = prompt.chunk.tensors[1]
+    prompt.extend(0, 1, None, None, None, None, None)
+    for t in (prompt.pages.arena, prompt.table, prompt.workspace, lens):
+        assert "side" in t.streams
+        t.streams.clear()
+    prompt.read(DeviceTensor(), DeviceTensor())
+    for t in (prompt.pages.arena, prompt.table, lens):
+        assert "side" in t.streams
