@@ -148,10 +148,12 @@ class PagedPrompt:
         self.device = self.pages.arena.device
         self.workspace = None
         self.chunk = None
+        self.before = None                    # (tokens, chunk) that drop_chunk() goes back to
 
     def begin_chunk(self, new_tokens) -> V.vlc_chunk:
         """The next chunk brings new_tokens[b] tokens to request b (0: none): the lengths that extend() and the calls on
-        self.chunk take from here on."""
+        self.chunk take from here on, and what self.tokens counts.  An extend() that is refused may be repeated; a chunk whose rows
+        will not come is taken back by drop_chunk().  Copies the lengths to the device, which waits for the current stream."""
         new = [int(c) for c in new_tokens]
         if len(new) != len(self.tokens) or min(new) < 0 or max(new) < 1:
             raise ValueError("new_tokens: a count for each request, none negative and not all zero")
@@ -159,9 +161,18 @@ class PagedPrompt:
         if max(total) > self.max_len:
             raise ValueError(f"a request would hold {max(total)} tokens, {self.max_len} were provided for")
         lens = torch.tensor(list(zip(total, new)), dtype=torch.int32).to(self.device)
-        self.chunk = V.make_chunk(self.table, max(new), max(total), lens)
-        self.tokens = total
+        chunk = V.make_chunk(self.table, max(new), max(total), lens)
+        self.before = (self.tokens, self.chunk)
+        self.tokens, self.chunk = total, chunk
         return self.chunk
+
+    def drop_chunk(self) -> None:
+        """Takes the last begin_chunk() back, so that the next chunk starts where that one did: positions that were counted but
+        never written would be attended as if they had been.  Once for each begin_chunk()."""
+        if self.before is None:
+            raise ValueError("no chunk to take back")
+        self.tokens, self.chunk = self.before
+        self.before = None
 
     def _used(self, *tensors) -> None:
         """The pages, the table and these own tensors are used on the current stream, which may be another than the one they were

@@ -27,7 +27,7 @@ def prompt(V, monkeypatch):
     """A prompt of two requests with room for 100 tokens whose library calls do nothing but can be made to fail."""
     from paper_2410_23317_amd import pipeline
     p = object.__new__(pipeline.PagedPrompt)
-    p.max_len, p.tokens, p.chunk, p.workspace, p.device = 100, [0, 0], None, DeviceTensor(), torch.device("cpu")
+    p.max_len, p.tokens, p.chunk, p.before, p.workspace, p.device = 100, [0, 0], None, None, DeviceTensor(), torch.device("cpu")
     p.table, p.pages = DeviceTensor(), SimpleNamespace(arena=DeviceTensor(), shape=SimpleNamespace(L=1))
     p.calls, p.fail = [], False
 
@@ -58,3 +58,31 @@ def test_everything_a_call_works_on_is_recorded_on_its_stream(prompt):
     prompt.read(DeviceTensor(), DeviceTensor())
     for t in (prompt.pages.arena, prompt.table, lens):
         assert "side" in t.streams
+
+
+def test_a_chunk_that_does_not_come_is_taken_back(prompt):
+    """A refused extend() may be repeated; drop_chunk() leaves no counted positions behind, and the earlier chunk in force."""
+    with pytest.raises(ValueError):
+        prompt.drop_chunk()
+    first = prompt.begin_chunk([3, 5])
+    prompt.extend(0, 1, None, None, None, None, None)
+    prompt.begin_chunk([10, 0])
+    prompt.fail = True
+    with pytest.raises(ValueError, match="vlc_pages"):
+        prompt.extend(0, 1, None, None, None, None, None)
+    assert prompt.tokens == [13, 5]                              # the same chunk again would be the same positions
+    prompt.fail = False
+    prompt.extend(0, 1, None, None, None, None, None)
+    prompt.begin_chunk([1, 1])
+    prompt.drop_chunk()
+    assert prompt.tokens == [13, 5] and prompt.chunk.lens == [[13, 10], [5, 0]]
+    with pytest.raises(ValueError):
+        prompt.drop_chunk()                                      # that chunk's rows are in the pages
+    prompt.begin_chunk([2, 0])
+    assert prompt.chunk.lens == [[15, 2], [5, 0]] and prompt.chunk is not first
+    with pytest.raises(ValueError):
+        prompt.begin_chunk([100, 0])                             # refused: nothing changes
+    assert prompt.tokens == [15, 5] and prompt.chunk.lens == [[15, 2], [5, 0]]
+    prompt.drop_chunk()
+    prompt.begin_chunk([1, 7])
+    assert prompt.chunk.lens == [[14, 1], [12, 7]]
