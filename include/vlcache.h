@@ -497,7 +497,9 @@ vlc_status vlc_pages_read(vlc_pages* pages, const vlc_chunk* chunk, int32_t laye
  *   out[l,b,h,i,:] = sum_j exp(s_ij - M_i) V_j / Z_i,   M_i = max_j s_ij,  Z_i = sum_j exp(s_ij - M_i)
  *
  * A position that a row does not see has no influence on it, whatever it holds.  Logits of -inf weigh nothing; a row with
- * nothing else is 0 with M = -inf, Z = 0.
+ * nothing else is 0 with M = -inf, Z = 0.  A number of V that is not finite spoils that output, and no other, of the rows that
+ * see it and have a logit above -inf: a NaN makes it NaN; an infinity makes it that infinity if its weight exp(s - M) is at least 2^-100
+ * (and no other one is of the other sign), else it is not finite, infinity or NaN by where the position lies.
  * q, out       [layers in range, B, Hq, max_new, d], storage dtype; rows >= c_b are not read / left as they are
  * k_new, v_new [layers in range, B, Hkv, max_new, d], or both NULL
  * sm_scale     [L] float (indexed by absolute layer), any finite numbers, or NULL for 1/sqrt(d)

@@ -80,3 +80,45 @@ def test_a_prompt_dropped_while_a_stream_works_on_it_keeps_its_memory():
     later = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(4)]
     assert busy and was not in [t.data_ptr() for t in later]
     side.synchronize()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cn", [1, 3, 8, 17, 30, 40, 300])
+def test_infinities_of_v_whose_weight_is_small(dtype, cn):
+    """Logits of -60, -200 and -inf among logits of 0, in tiles that all rows see to their end and in the last ones: an infinity
+    of weight e^-60 is that infinity, one that weighs too little for a number is not finite, and NaN is NaN."""
+    n, d, inf, nan = cn + 700, 64, float("inf"), float("nan")
+    spots = [(3, -60.0, inf), (200, -60.0, -inf), (201, -200.0, inf), (202, -inf, inf), (203, -200.0, nan), (204, -inf, nan),
+             (690, -60.0, inf), (691, -200.0, -inf), (692, -inf, inf), (693, -200.0, nan), (694, -inf, nan),
+             (700, -60.0, -inf), (700 + cn // 2, -200.0, inf), (n - 1, -60.0, inf)]
+    spots = list({t: (t, s, x) for t, s, x in spots}.values())
+
+    def edit(k, v):
+        k[..., :] = 0
+        for e, (t, s, x) in enumerate(spots):
+            k[:, :, :, t, 0] = s
+            v[:, :, :, t, e] = x
+    c = U.Case(1, 4, 2, d, [(n, cn)], ps=16, dtype=dtype, k_edit=edit)
+    c.q.zero_()
+    c.q[..., 0] = 1
+    one = torch.ones(1, device="cuda")
+    for fresh in (False, True):
+        if fresh:
+            c.pages.arena[c.pages.layout.k_off:] = 255
+            c.fill([700])
+        else:
+            c.fill()
+        out, _, _ = c.attn(fresh=fresh, scale=one)
+        torch.cuda.synchronize()
+        got = out[0, 0, :, :cn].float().cpu()
+        for e, (t, s, x) in enumerate(spots):
+            first = max(t - 700, 0)                              # first row of the chunk that sees it
+            assert bool(torch.isfinite(got[:, :first, e]).all()), (t, s, x)
+            seen = got[:, first:, e]
+            if x != x:
+                assert bool(torch.isnan(seen).all()), (t, s, x)
+            elif s == -60.0:
+                assert bool((seen == x).all()), (t, s, x)
+            else:
+                assert not bool(torch.isfinite(seen).any()), (t, s, x)
+        assert bool(torch.isfinite(got[..., len(spots):]).all())
