@@ -510,8 +510,8 @@ vlc_status vlc_pages_read(vlc_pages* pages, const vlc_chunk* chunk, int32_t laye
  *              vlc_pages that may overlap on the device race, as those on one vlc_cache do.
  * Accumulation and statistics are fp32; bf16 storage rounds the probabilities (of codes: times V's scale) to bf16 for the
  * product with V, or for few rows to a sum of two bf16 numbers; fp32 storage does not.  Weights are held relative to a
- * number near M, and are at most 2^10 before the division: V of magnitudes between 2^-100 and 2^100 is safe from
- * underflow and overflow on the way.
+ * number near M, and are at most 2^10 before the division: V of magnitudes between 2^-100 and 2^117 / n is safe from underflow
+ * and overflow on the way, n being the request's tokens (2^92 at the most that a call takes, 2^102 up to 32768).
  */
 typedef struct {
     float* row_max;

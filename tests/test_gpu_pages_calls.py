@@ -122,3 +122,30 @@ def test_infinities_of_v_whose_weight_is_small(dtype, cn):
             else:
                 assert not bool(torch.isfinite(seen).any()), (t, s, x)
         assert bool(torch.isfinite(got[..., len(spots):]).all())
+
+
+@pytest.mark.parametrize("fmt", ["plain", "fp8", "int8"])
+@pytest.mark.parametrize("d,B", [(128, 256), (64, 512)])
+def test_large_v_under_many_weights_above_one(fmt, d, B):
+    """V of 2^98 over 300000 keys that all weigh 2^9.9 of the first 32, which set what the weights are relative to: sums of 2^126.1.
+    The output is a mean of equal numbers: wrong by the rounding of the weight and its own (half a step each, 2^-8) and by
+    what 300000 / 16 sums of equal numbers lose, 2^-25 each."""
+    import math
+    import paper_2410_23317_amd as V
+    n, cn, ps = 300000, 65, 256
+    pages = V.vlc_pages_create(V.make_pages_shape(1, 1, 1, d, ps, -(-n // ps), "bf16", fmt))
+    k = torch.zeros((1, 1, 1, n, d), dtype=torch.bfloat16, device="cuda")
+    k[..., 32:, 0] = 9.875
+    sign = torch.ones(d, dtype=torch.bfloat16, device="cuda")
+    sign[::3] = -1
+    v = (sign * 2.0 ** 98).expand(1, 1, 1, n, d)
+    table = torch.arange(-(-n // ps), dtype=torch.int32, device="cuda")[None]
+    V.vlc_pages_write(pages, V.make_chunk(table, n, n), 0, 1, k, v)
+    chunk = V.make_chunk(table.expand(B, -1).contiguous(), cn, n)            # every request has the same pages
+    assert V.vlc_pages_attn_workspace_bytes(pages, chunk, 1) == 0            # one split, so one first 32 keys
+    q = torch.zeros((1, B, 1, cn, d), dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 1
+    out = torch.empty_like(q)
+    V.vlc_pages_attn(pages, chunk, 0, 1, q, None, None, torch.full((1,), math.log(2.0), device="cuda"), out, None, None, None)
+    V.vlc_pages_status(pages)
+    U.within(out, (sign * 2.0 ** 98).double().cpu().expand(out.shape), 2.0 ** 98 * (2 * 2.0 ** -8 + 2 * n / 16 * 2.0 ** -25), "mean")
