@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import pages_util as U
+import test_gpu_pages as P
 
 pytestmark = pytest.mark.gpu
 
@@ -149,3 +150,169 @@ def test_large_v_under_many_weights_above_one(fmt, d, B):
     V.vlc_pages_attn(pages, chunk, 0, 1, q, None, None, torch.full((1,), math.log(2.0), device="cuda"), out, None, None, None)
     V.vlc_pages_status(pages)
     U.within(out, (sign * 2.0 ** 98).double().cpu().expand(out.shape), 2.0 ** 98 * (2 * 2.0 ** -8 + 2 * n / 16 * 2.0 ** -25), "mean")
+
+
+# Forms of the kernels that the shapes of test_attention_of_a_chunk do not reach: 49 to 64 rows of a KV head in one and in several
+# units of keys, 33 to 48 rows in several.
+FEW_ROWS = [                                                     # Hq, Hkv, d, ps, lens
+    (7, 1, 64, 16, [(400, 9), (13, 9), (9, 9)]),
+    (7, 1, 128, 32, [(333, 9), (50, 2)]),
+    (14, 2, 64, 64, [(1700, 9), (520, 5), (100, 9)]),
+    (7, 1, 128, 16, [(1901, 9), (64, 8)]),
+    (2, 2, 64, 16, [(64, 64), (300, 64)]),
+    (1, 1, 64, 32, [(1203, 64), (65, 50)]),
+    (1, 1, 128, 128, [(490, 64), (64, 64)]),
+    (3, 3, 128, 16, [(1500, 64), (900, 49)]),
+    (7, 1, 64, 32, [(1333, 5), (600, 5)]),                       # 35 rows
+    (14, 2, 128, 16, [(2050, 5), (30, 3)]),
+    (8, 1, 64, 16, [(1100, 6), (700, 1)]),                       # 48 rows
+    (4, 1, 128, 256, [(1537, 12), (513, 12)]),
+]
+
+
+@pytest.mark.parametrize("fmt,dtype", U.FORMATS)
+@pytest.mark.parametrize("Hq,Hkv,d,ps,lens", FEW_ROWS)
+def test_33_to_64_rows_of_a_kv_head(fmt, dtype, Hq, Hkv, d, ps, lens):
+    P.test_attention_of_a_chunk(fmt, dtype, 1, Hq, Hkv, d, ps, lens)
+
+
+# A block that walks more pages than a wave holds ids of (64): all keys in one split, and several splits of more than 64 pages.
+LONG_WALKS = [                                                   # L, Hq, Hkv, d, lens, one split
+    (2, 64, 64, 128, [(2100, 70), (1100, 70)], True),            # up to 128 rows: four waves of 32
+    (2, 128, 64, 128, [(2100, 70), (1100, 33)], True),           # up to 256: eight waves
+    (4, 64, 64, 64, [(2100, 70), (1030, 70)], True),
+    (4, 128, 64, 64, [(1500, 70), (1100, 70)], True),            # two blocks of 32 rows a wave
+    (1, 64, 32, 128, [(6000, 70), (3500, 70)], False),
+    (2, 64, 32, 64, [(6000, 70), (3500, 70)], False),
+]
+
+
+@pytest.mark.parametrize("fmt", ["plain", "fp8", "int8"])
+@pytest.mark.parametrize("stats", [False, True])
+@pytest.mark.parametrize("L,Hq,Hkv,d,lens,one", LONG_WALKS)
+def test_blocks_that_walk_more_than_64_pages(fmt, stats, L, Hq, Hkv, d, lens, one):
+    import paper_2410_23317_amd as V
+    c = U.Case(L, Hq, Hkv, d, lens, ps=16, fmt=fmt)
+    c.fill()
+    assert (V.vlc_pages_attn_workspace_bytes(c.pages, c.chunk, L) == 0) == one
+    out, M, Z = c.attn(stats=stats)
+    V.vlc_pages_status(c.pages)
+    c.check(out, M, Z, "walk", stats=stats)
+
+
+@pytest.mark.parametrize("fmt,dtype", U.FORMATS)
+@pytest.mark.parametrize("lens,attend", [([(50, 7), (33, 0), (20, 20)], False), ([(50, 3), (33, 0), (9, 9)], True), ([(150, 50), (33, 0), (70, 70)], True)])
+def test_every_other_byte_of_the_pages_stays(fmt, dtype, lens, attend):
+    """Layer 1 of 2 is written, by a write or by the attention of a few or of many rows; the rows behind a request's own are
+    finite numbers that the arena does not hold.  Byte by byte, nothing but the chunk's slots has changed."""
+    from types import SimpleNamespace
+    import paper_2410_23317_amd as V
+    from paper_2410_23317_amd.pipeline import pages_layer_view
+    c = P.rows_case(2, 2, 64, lens, 16, fmt, dtype)
+    c.fill([n - k for n, k in lens])
+    before = c.pages.arena.clone()
+    rows = []
+    for x, t in zip((c.k, c.v), c.new_rows()):
+        for b, (n, k) in enumerate(lens):
+            t[:, b, :, k:] = 3.0
+        rows.append(t[1:])
+    if attend:
+        out = torch.empty_like(c.q[1:])
+        ws = torch.empty(V.vlc_pages_attn_workspace_bytes(c.pages, c.chunk, 1), dtype=torch.uint8, device="cuda")
+        V.vlc_pages_attn(c.pages, c.chunk, 1, 2, c.q[1:], *rows, c.scale, out, None, None, ws)
+    else:
+        V.vlc_pages_write(c.pages, c.chunk, 1, 2, *rows)
+    V.vlc_pages_status(c.pages)
+    now, table, k_off = c.pages.arena.clone(), c.table.cpu(), c.pages.layout.k_off
+    assert not torch.equal(now, before)
+    for arena in (now, before):
+        for x in pages_layer_view(SimpleNamespace(shape=c.pages.shape, layout=c.pages.layout, arena=arena), 1):
+            for b, (n, k) in enumerate(lens):
+                for t in range(n - k, n):
+                    x[int(table[b, t // 16]), :, t % 16] = 0
+    assert torch.equal(now[k_off:], before[k_off:])
+    ko, vo = torch.zeros_like(c.k), torch.zeros_like(c.v)
+    V.vlc_pages_read(c.pages, c.chunk, 1, 2, 0, ko[1:], vo[1:])
+    for got, src in ((ko, c.k), (vo, c.v)):
+        for b, (n, _) in enumerate(lens):
+            assert torch.equal(got[1, b, :, :n].cpu(), U.held(src[1, b, :, :n], fmt).float().to(U.storage(dtype)))
+
+
+@pytest.mark.parametrize("fmt,dtype,d", [("plain", "bf16", 128), ("plain", "f32", 64), ("fp8", "bf16", 128), ("int8", "bf16", 64)])
+def test_what_a_prompt_in_chunks_leaves_for_decoding(fmt, dtype, d):
+    """Statistics, scores, kept positions and decode outputs of the compression, each against 64 bits from what came before it: no
+    comparison depends on another one's outcome.  Scores of quantised pages: the read rounds K to bf16, half a step of 2^-8
+    of every term of a logit; statistics are those of the pages' own numbers."""
+    import math
+    from oracle import vlcache_oracle as O
+    import paper_2410_23317_amd as V
+    from paper_2410_23317_amd.pipeline import PagedPrompt, VLCachePath
+    L, B, Hq, Hkv, tau = 2, 2, 8, 2, 20
+    g, m_b, tau_b = Hq // Hkv, [640, 411], [20, 13]
+    m, dt = max(m_b), U.storage(dtype)
+    gen = torch.Generator().manual_seed(17)
+    k, v = (torch.randn((B, L, Hkv, m, d), generator=gen).to(dt).cuda() for _ in range(2))
+    k[:, :, :, 60:64] *= 4
+    q = torch.randn((B, L, Hq, m, d), generator=gen).to(dt).cuda()
+    sm = torch.tensor([0.8, 1.3], device="cuda") / math.sqrt(d)
+    lens = torch.tensor(list(zip(m_b, tau_b)), dtype=torch.int32, device="cuda")
+    path = VLCachePath(V.make_shape(B, L, Hq, Hkv, d, m, tau, dtype, lens=lens), T_max=4, want_idx=True, lens=lens)
+    prompt = PagedPrompt(L, Hq, Hkv, d, dtype, B, m, page_slots=16, format=fmt)
+    prompt.begin_chunk([9, 9])
+    prompt.drop_chunk()                                          # never came
+    q_win = torch.zeros((B, L, Hq, tau, d), dtype=dt, device="cuda")
+    for chunk in ([500, 1], [120, 397], tau_b):
+        prompt.begin_chunk(chunk)
+        c = max(chunk)
+        rows = [torch.zeros((B, L, x.shape[2], c, d), dtype=dt, device="cuda") for x in (q, k, v)]
+        for t, x in zip(rows, (q, k, v)):
+            for b, (n, cb) in enumerate(zip(prompt.tokens, chunk)):
+                t[b, :, :, :cb] = x[b, :, :, n - cb: n]
+        last = chunk is tau_b
+        if last:
+            q_win.copy_(rows[0])
+        rows = [t.transpose(0, 1) for t in rows]
+        stats = [x.transpose(0, 1) for x in (path.row_max, path.row_sum)] if last else []
+        prompt.extend(0, L, *rows, sm, torch.empty_like(rows[0]), *stats)
+    k_read, v_read = torch.zeros_like(k), torch.zeros_like(v)
+    prompt.compress(path, q_win, sm, k_read, v_read)
+    prompt.status()
+    path.status()
+    torch.cuda.synchronize()
+    scores = path.scores.double().cpu()
+    kept = {}
+    for b in range(B):
+        n, c = m_b[b], tau_b[b]
+        hidden = torch.arange(n)[None, :] > torch.arange(n - c, n)[:, None]
+        for l in range(L):
+            at, scale = f"request {b} layer {l}", sm[l].item()
+            K, Vs = U.held(k[b, l, :, :n], fmt), U.held(v[b, l, :, :n], fmt)
+            ref = U.attention(q_win[b, l, :, :c], K, Vs, scale, n, c)
+            _, bm, bz = U.bounds(ref, dtype, d, n)
+            U.within(path.row_max[b, l, :, :c], ref[1], bm, at + " max")
+            U.within(path.row_sum[b, l, :, :c], ref[2], bz * ref[2], at + " sum")
+            for h in range(Hkv):
+                qh = q_win[b, l, h * g: (h + 1) * g, :c].double().cpu()
+                w = torch.exp((qh @ K[h].T * scale).masked_fill(hidden, -math.inf) - ref[1][h * g: (h + 1) * g, :, None])
+                w = w / ref[2][h * g: (h + 1) * g, :, None]
+                moved = (0.0 if fmt == "plain" else 2.0 ** -8) * scale * (qh.abs() @ K[h].abs().T)
+                each = moved + (bm + bz)[h * g: (h + 1) * g, :, None] + (d + 8) * 2.0 ** -24 * ref[4][h * g: (h + 1) * g, :, None] + 2.0 ** -20
+                U.within(scores[b, l, h, :n], w.sum((0, 1)), (w * torch.expm1(each)).sum((0, 1)) + 1e-7, f"{at} head {h} scores")
+                kl = int(path.k[b, l])
+                idx = path.idx_out[b, l, h, :kl].cpu().numpy()
+                assert (idx == O.topk(path.scores[b, l, h, :n].cpu().numpy(), kl)).all(), at
+                kept[b, l, h] = torch.from_numpy(idx).long()
+    grown = {(b, l): [] for b in range(B) for l in range(L)}
+    o = torch.empty((L, B, Hq, d), dtype=dt, device="cuda")
+    for step in range(3):
+        qs, kn, vn = [torch.randn((L, B, h, d), generator=gen).to(dt).cuda() for h in (Hq, Hkv, Hkv)]
+        path.decode(0, L, qs, kn, vn, sm, o)
+        path.status()
+        for (b, l), new in grown.items():
+            new.append((kn[l, b], vn[l, b]))
+            for h in range(Hkv):
+                rows = kept[b, l, h].cuda()
+                K, Vs = (torch.cat([x[b, l, h][rows], torch.stack([y[i][h] for y in new])]).double().cpu()[None] for i, x in ((0, k_read), (1, v_read)))
+                n = K.shape[1]
+                ref = U.attention(qs[l, b, h * g: (h + 1) * g, None], K, Vs, sm[l].item(), n, 1)
+                U.within(o[l, b, h * g: (h + 1) * g, None], ref[0], U.bounds(ref, dtype, d, n)[0], f"step {step} request {b} layer {l} head {h}")
