@@ -162,6 +162,7 @@ class PagedPrompt:
             raise ValueError(f"a request would hold {max(total)} tokens, {self.max_len} were provided for")
         lens = torch.tensor(list(zip(total, new)), dtype=torch.int32).to(self.device)
         chunk = V.make_chunk(self.table, max(new), max(total), lens)
+        chunk.new_tokens = new
         self.before = (self.tokens, self.chunk)
         self.tokens, self.chunk = total, chunk
         return self.chunk
@@ -200,13 +201,27 @@ class PagedPrompt:
         """Every request's K and V so far, into tensors [B, L, Hkv, m, d]; rows beyond a request's are left as they are."""
         if self.chunk is None:
             raise ValueError("begin_chunk() comes first")
+        if k_out.shape[3] < max(self.tokens):
+            raise ValueError(f"k_out and v_out have {k_out.shape[3]} rows, a request holds {max(self.tokens)} tokens")
         self._used(self.chunk.tensors[1])
         V.vlc_pages_read(self.pages, self.chunk, 0, self.pages.shape.L, 0, k_out.transpose(0, 1), v_out.transpose(0, 1))
 
     def compress(self, path: VLCachePath, q_win, sm_scale, k_out, v_out) -> None:
         """Compression of the prompts whose last chunk was the window and left its statistics in path.row_max and
         path.row_sum (extend(.., row_max=path.row_max.transpose(0, 1), row_sum=..)); path.shape.lens, if the batch is
-        ragged, holds what self.chunk.lens holds."""
+        ragged, holds what self.chunk.lens holds.  Scores of quantised pages are formed with K as the read rounds it to the storage
+        type, under statistics of the codes' own values."""
+        if self.chunk is None:
+            raise ValueError("begin_chunk() comes first")
+        s = path.shape
+        for name, t, dims in (("q_win", q_win, (s.B, s.L, s.Hq, s.tau, s.d)), ("k_out", k_out, (s.B, s.L, s.Hkv, s.m, s.d)),
+                              ("v_out", v_out, (s.B, s.L, s.Hkv, s.m, s.d))):
+            if tuple(t.shape) != dims:
+                raise ValueError(f"{name} must have the path's shape {dims}, not {tuple(t.shape)}")
+        if self.chunk.max_new != s.tau:
+            raise ValueError(f"the last chunk, of up to {self.chunk.max_new} tokens, is not the path's window of {s.tau}")
+        if not s.lens and (min(self.tokens) != s.m or min(self.chunk.new_tokens) != s.tau):
+            raise ValueError("requests of different lengths or windows need their pairs in path.shape.lens")
         self.read(k_out, v_out)
         path.score_from_stats(q_win, k_out, sm_scale)
         V.vlc_sparsity_allocate(path.shape, path.nnz, path.gamma, path.alpha[0], path.alpha[1], path.k, path.beta)

@@ -9,14 +9,14 @@ from test_pages_abi import V  # noqa: F401
 
 
 class DeviceTensor:
-    def __init__(self, n=1 << 20):
-        self.n, self.streams = n, []
+    def __init__(self, *shape):
+        self.shape, self.streams = shape, []
 
     def record_stream(self, s):
         self.streams.append(s)
 
     def numel(self):
-        return self.n
+        return 1 << 20
 
     def transpose(self, *a):
         return self
@@ -55,7 +55,7 @@ def test_everything_a_call_works_on_is_recorded_on_its_stream(prompt):
     for t in (prompt.pages.arena, prompt.table, prompt.workspace, lens):
         assert "side" in t.streams
         t.streams.clear()
-    prompt.read(DeviceTensor(), DeviceTensor())
+    prompt.read(DeviceTensor(2, 1, 1, 100, 64), DeviceTensor(2, 1, 1, 100, 64))
     for t in (prompt.pages.arena, prompt.table, lens):
         assert "side" in t.streams
 
@@ -86,3 +86,42 @@ def test_a_chunk_that_does_not_come_is_taken_back(prompt):
     prompt.drop_chunk()
     prompt.begin_chunk([1, 7])
     assert prompt.chunk.lens == [[14, 1], [12, 7]]
+
+
+def test_tensors_that_do_not_fit_the_prompt_are_refused(prompt, monkeypatch):
+    """A read that would leave tokens out, and a compression whose tensors, window or lengths are not the prompt's: the calls
+    behind it take bare pointers."""
+    from paper_2410_23317_amd import pipeline
+    B, L, Hq, Hkv, d, m, tau = 2, 1, 4, 2, 64, 60, 8
+    t = DeviceTensor
+    path = SimpleNamespace(shape=SimpleNamespace(B=B, L=L, Hq=Hq, Hkv=Hkv, d=d, m=m, tau=tau, lens=None), score_from_stats=lambda *a: prompt.calls.append("score"),
+                           topk_compact=lambda *a: prompt.calls.append("compact"), nnz=None, gamma=None, alpha=(1, 10), k=None, beta=None)
+    monkeypatch.setattr(pipeline.V, "vlc_sparsity_allocate", lambda *a: prompt.calls.append("allocate"))
+    q, kv = t(B, L, Hq, tau, d), t(B, L, Hkv, m, d)
+
+    def compress(q=q, k=kv, v=kv):
+        prompt.calls.clear()
+        prompt.compress(path, q, None, k, v)
+    with pytest.raises(ValueError, match="begin_chunk"):
+        compress()
+    prompt.begin_chunk([52, 52])
+    with pytest.raises(ValueError, match="window"):
+        compress()
+    prompt.begin_chunk([8, 8])
+    compress()
+    assert prompt.calls == ["vlc_pages_read", "score", "allocate", "compact"]
+    for kw in (dict(q=t(B, L, Hq, tau + 1, d)), dict(k=t(B, L, Hkv, m + 1, d)), dict(v=t(B, L, Hkv, m - 1, d)), dict(k=t(L, B, Hkv, m, d))):
+        with pytest.raises(ValueError, match="shape"):
+            compress(**kw)
+    prompt.drop_chunk()
+    for new in ([8, 7], [7, 8]):
+        prompt.begin_chunk(new)
+        with pytest.raises(ValueError, match="lens"):
+            compress()
+        prompt.drop_chunk()
+    path.shape.lens = 4096
+    prompt.begin_chunk([8, 7])
+    compress()
+    prompt.read(t(B, L, Hkv, 60, d), t(B, L, Hkv, 60, d))
+    with pytest.raises(ValueError, match="59 rows"):
+        prompt.read(t(B, L, Hkv, 59, d), t(B, L, Hkv, 59, d))
