@@ -211,7 +211,7 @@ struct PagesAttn {
     vlc_row_stats stats;               // row_max null: none
     void* workspace;
 };
-// at most 32 query rows per KV head (pages_attn_few.hip); writes the chunk's rows itself
+// at most 64 query rows per KV head, fp32 storage 32 (pages_attn_few.hip); writes the chunk's rows itself
 bool pages_few_supported(const PagesCall& c);
 size_t pages_few_workspace_bytes(const PagesCall& c);
 hipError_t launch_pages_few(const PagesAttn& a);

@@ -103,7 +103,9 @@ __device__ __forceinline__ uint32_t row_absmax_bits(const uint4& v) {
     for (int o = LPR / 2; o >= 1; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, kWave));
     return m;
 }
-// 8 codes and the row's scale; a row with a NaN or an infinity has codes of 0 and a scale of NaN.
+// 8 codes and the row's scale; a row with a NaN or an infinity has codes of 0 and a scale of NaN.  (Finite rows of FP8 pages are the
+// codes and scales of quantize_row_e4m3, which the compressed cache has and which drops a NaN from the maximum: rows here are read
+// back, so such a row has to stay one.)
 template <int FMT, int LPR>
 __device__ __forceinline__ uint2 quantize_page_row(const uint4& v, float& scale) {
     constexpr float kTop = FMT == kPageFp8 ? 448.0f : 127.0f;

@@ -2,8 +2,9 @@
 // heads of up to 64 / g tokens, which is decoding, and verifying drafted tokens.
 //
 // Bound by memory where there is enough of it: every K and V row is read once and serves all query rows of its KV head (24 FP8
-// requests of up to 10369 positions, 287 MB, 55 us: 5.2 TB/s).  A small call is a chain of waits: one token over 2945 positions (12
-// MB) takes 9.1 us, over 100 positions 6.4.  A (layer, request, KV head) row of the cache is cut into units of 2^unit_shift
+// requests of up to 10369 positions, 287 MB, take 65.6 us on inputs that no cache holds: 4.4 TB/s; 53 to 56 on the same input again,
+// which the memory-side cache partly holds; plain rows 114 us, 4.9 TB/s).  A small call is a chain of waits: one token over 2945
+// positions (12 MB) takes 10.0 us, over 300 8.4, over 100 6.5.  A (layer, request, KV head) row of the cache is cut into units of 2^unit_shift
 // positions, a block of four waves each; the tiles of a unit are dealt to the waves, which merge through LDS.  Units of a row
 // leave unnormalised partial results.  Up to 16 query rows they store them with device scope and count themselves; the one
 // that counts last merges them and writes the output (its own stores are acknowledged before it counts, so whoever counts last
@@ -14,7 +15,7 @@
 //
 // A tile's operands come from memory in the order the matrix instructions want, without a trip through LDS or across
 // lanes.  bf16 (codes are expanded to bf16, exactly, where they are used; K's scale multiplies the finished logit, V's the
-// probability before it is rounded to bf16): 32 positions, 8 G + j for lane group G = lane / 16, place j.  Logits
+// probability before it is split into two bf16 numbers): 32 positions, 8 G + j for lane group G = lane / 16, place j.  Logits
 // S^T[position][column] = K Q^T, a column being a query row; a lane fetches the K pieces of the position whose logit comes
 // out for its own group, holds 8 logits of one column, and their probabilities are the second product's operand as they
 // are; V's operand is a transpose inside the lane (one v_perm_b32 per register) of the rows it fetched.
@@ -716,7 +717,8 @@ FewPlan plan(const PagesCall& c) {
     // more blocks than that, 1024, which balance requests of different lengths better.  us of one layer, eight KV heads of four
     // query heads, units of 128 / 256 / 512 / 1024 / 2048: one request of 2945 positions 10.1 / 9.1 / 11.0 / 15.4 / 23.3, of 300
     // 8.7 / 8.8 / 8.2, of 1000 9.3 / 10.1 / 12.3 (so 128 up to 64 positions a block), of 10000 19.7 / 15.4 / 13.7 / 16.2 / 24.7, of 32768 48.4 / 33.4 / 27.9 / 25.6 / 25.5;
-    // four of 10368 48.6 / 35.3 / 31.9 / 32.7 / 29.0; 24 of up to 10369 (FP8) 99.5 / 67.3 / 53.7 / 54.7 / 57.3.
+    // four of 10368 48.6 / 35.3 / 31.9 / 32.7 / 29.0; 24 of up to 10369 (FP8) 99.5 / 67.3 / 53.7 / 54.7 / 57.3.  (The same input again
+    // and again; all but the last of plain rows of 128.  The rule counts positions: shorter rows, of codes or of 64 numbers, have the same units.)
     const int64_t per_block = rows * c.chunk.max_len / 192;
     f.unit_shift = per_block > 64 ? 8 : 7;
     while (f.unit_shift < 11 && per_block * 10 > (int64_t)14 << f.unit_shift) ++f.unit_shift;

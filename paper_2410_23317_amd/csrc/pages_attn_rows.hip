@@ -12,12 +12,14 @@
 // j + 1.  Between waves, every SIMD holds two, which cover each other's waits: eight waves of 32 rows share the keys of a
 // block of 128-wide heads, and two blocks of four waves of 64 rows fit a compute unit with 64-wide ones.  2048 tokens of 32
 // heads over 32768 keys, us (TFLOP/s): d = 128 one wave per SIMD with 64 rows 1028, two with 32 rows 993 (1073); d = 64 one 811,
-// two 588 (905).  A large bf16 matrix product reaches 1256 TFLOP/s here; neither more lookahead, other wave priorities nor
-// none of the lookahead moves the 993 by 1 %.  FP8 pages 1144, int8 about 1190 (d = 64: 781): the codes' expansion, two scales, and
-// the sum over rounded weights (see step; 5 % of the time with d = 128, 13 % with 64).
+// two 588 (905).  A large bf16 matrix product reached 1256 TFLOP/s on that card (1308 on another); neither more lookahead, other wave
+// priorities nor none of the lookahead moves the 993 by 1 %.  With 64-wide heads a logit is worth half the products, and the vector unit is
+// what is busy: 68 % of the cycles, the matrix unit 44 (d = 128: 50 and 55).  FP8 pages 1144, int8 about 1190 (d = 64: 781 and 799): the
+// codes' expansion, two scales, and the sum over rounded weights (see step; 5 % of the time with d = 128, 13 % with 64).  The eight-wave
+// instances for codes keep two registers in scratch, 12 bytes a lane, from before the first loop to between the two.
 //
-// A row's weights are relative to m, which starts as the maximum of its first 32 keys and is raised only when a logit exceeds
-// it by more than 2^kSlack: the weights are then at most 2^kSlack instead of 1, and the accumulators are rescaled a few times per
+// A row's weights are relative to m, which starts as the maximum of its first 32 keys and is raised only when a logit (base 2)
+// exceeds it by more than kSlack: the weights are then at most 2^kSlack instead of 1, and the accumulators are rescaled a few times per
 // row instead of at every new maximum.  The rescaling stands outside the loop over the steps; inside, the accumulators had two
 // definitions and were copied between registers at every step (1372 us instead of 1050).
 //
@@ -63,7 +65,7 @@ __device__ __forceinline__ float max_across_halves(float x) {
 }
 
 // STATS: pages of codes keep the plain sum of the weights too, which only calls that ask for statistics pay (d = 64, two blocks of
-// rows a wave: 877 us instead of 781; one block a wave 1000 and more).
+// rows a wave, 42 registers in scratch: int8 905 us instead of 799; one block a wave 1000 and more).
 template <int D, int FMT, int RB, int W, bool STATS>
 __global__ __launch_bounds__(W * 64, 2) void pages_rows_kernel(PagesRowsParams ra) {
     constexpr int kWaves = W, kThreads = W * 64, kRows = 32 * RB * W;
