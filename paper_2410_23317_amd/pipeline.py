@@ -218,8 +218,8 @@ class PagedPrompt:
                               ("v_out", v_out, (s.B, s.L, s.Hkv, s.m, s.d))):
             if tuple(t.shape) != dims:
                 raise ValueError(f"{name} must have the path's shape {dims}, not {tuple(t.shape)}")
-        if self.chunk.max_new != s.tau:
-            raise ValueError(f"the last chunk, of up to {self.chunk.max_new} tokens, is not the path's window of {s.tau}")
+        if self.chunk.max_new > s.tau:
+            raise ValueError(f"the last chunk, of up to {self.chunk.max_new} tokens, is longer than the path's window of {s.tau}")
         if not s.lens and (min(self.tokens) != s.m or min(self.chunk.new_tokens) != s.tau):
             raise ValueError("requests of different lengths or windows need their pairs in path.shape.lens")
         self.read(k_out, v_out)

@@ -120,6 +120,10 @@ def test_tensors_that_do_not_fit_the_prompt_are_refused(prompt, monkeypatch):
             compress()
         prompt.drop_chunk()
     path.shape.lens = 4096
+    for new in ([8, 7], [5, 6]):                                 # windows below the path's tau, as the pairs of lens say
+        prompt.begin_chunk(new)
+        compress()
+        prompt.drop_chunk()
     prompt.begin_chunk([8, 7])
     compress()
     prompt.read(t(B, L, Hkv, 60, d), t(B, L, Hkv, 60, d))
